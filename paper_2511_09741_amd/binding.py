@@ -1,4 +1,4 @@
-"""ctypes binding over libtaw.so: the same names as include/taw.h and include/taw_ops.h.
+"""ctypes binding over libtaw.so: the same names as include/taw.h, include/taw_ops.h and include/model/taw_model.h.
 
 Argument marshalling only.  Device buffers are torch tensors (torch owns device memory and
 streams); every function takes their data pointers, calls the C entry point and raises TawError
@@ -19,6 +19,8 @@ TAW_ATTN_BWD_FUSED = 4
 TAW_ATTN_BWD_RECOMPUTE = 8
 TAW_IMPL_AUTO, TAW_IMPL_GENERIC, TAW_IMPL_MFMA, TAW_IMPL_MFMA_FUSED, TAW_IMPL_MFMA_ATOMIC, TAW_IMPL_MFMA_STORED = 0, 1, 2, 3, 4, 5
 TAW_GEMM_NT, TAW_GEMM_NN, TAW_GEMM_TN = 0, 1, 2
+TAW_I32, TAW_I64 = 0, 1
+TAW_LOSS_MEAN = 1
 TAW_OK = 0
 TAW_ERR_NULL, TAW_ERR_SHAPE, TAW_ERR_DTYPE, TAW_ERR_ALIGN, TAW_ERR_WORKSPACE, TAW_ERR_UNSUPPORTED, TAW_ERR_HIP = -1, -2, -3, -4, -5, -6, -7
 
@@ -38,6 +40,21 @@ class taw_weight_layout(C.Structure):
 class taw_adamw_desc(C.Structure):
     _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
                 ("weight_decay", C.c_float), ("grad_scale", C.c_float), ("step", C.c_int32), ("zero_grad", C.c_int32)]
+
+
+class taw_embed_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("T", C.c_int32), ("H", C.c_int32), ("V", C.c_int32), ("ld_table", C.c_int64), ("ld_x", C.c_int64),
+                ("scale", C.c_float), ("flags", C.c_uint32)]
+
+
+class taw_loss_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("grad_dtype", C.c_int32), ("T", C.c_int32), ("V", C.c_int32), ("V_pad", C.c_int32),
+                ("ld", C.c_int64), ("ld_grad", C.c_int64), ("label_smoothing", C.c_float), ("z_loss", C.c_float),
+                ("grad_scale", C.c_float), ("flags", C.c_uint32)]
+
+
+class taw_tensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("n", C.c_size_t), ("dtype", C.c_int32)]
 
 
 class taw_diag_rate(C.Structure):
@@ -110,6 +127,24 @@ _SIGS = {
     "taw_op_linear_bwd": (C.c_int, [_i32, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _i32, _vp]),
 }
 EXPORTS = tuple(_SIGS)
+# include/model/taw_model.h
+_ed, _ld, _tp = C.POINTER(taw_embed_desc), C.POINTER(taw_loss_desc), C.POINTER(taw_tensor)
+_MODEL_SIGS = {
+    "taw_embed_fwd": (C.c_int, [_ed, _vp, _i32, _vp, _vp, _vp]),
+    "taw_embed_bwd_workspace_bytes": (_sz, [_ed]),
+    "taw_embed_bwd": (C.c_int, [_ed, _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
+    "taw_loss_workspace_bytes": (_sz, [_ld]),
+    "taw_loss_fwd": (C.c_int, [_ld, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "taw_loss_fwd_bwd": (C.c_int, [_ld, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "taw_loss_bwd": (C.c_int, [_ld, _vp, _vp, _i32, _vp, _vp, _vp, _vp]),
+    "taw_grad_norm_workspace_bytes": (_sz, [_tp, _i32]),
+    "taw_grad_norm": (C.c_int, [_tp, _i32, _f, _f, _vp, _vp, _sz, _vp]),
+    "taw_grad_sumsq": (C.c_int, [_tp, _i32, _i32, _vp, _vp, _sz, _vp]),
+    "taw_clip_coef": (C.c_int, [_vp, _f, _f, _vp]),
+    "taw_grad_clip": (C.c_int, [_tp, _i32, _vp, _vp]),
+    "taw_optimizer_step_clipped": (C.c_int, [C.POINTER(taw_adamw_desc), _vp, _vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
+}
+MODEL_EXPORTS = tuple(_MODEL_SIGS)
 
 
 def load():
@@ -123,7 +158,7 @@ def load():
         # binds libtaw.so to that one; two HIP runtimes in one process do not both see the GPU.
         import torch  # noqa: F401
         lib = C.CDLL(LIB_PATH)
-        for name, (res, args) in _SIGS.items():
+        for name, (res, args) in {**_SIGS, **_MODEL_SIGS}.items():
             fn = getattr(lib, name)
             fn.restype, fn.argtypes = res, args
         _lib = lib
@@ -256,6 +291,138 @@ def taw_status_string(status: int) -> str:
 
 def taw_last_error() -> str:
     return load().taw_last_error().decode()
+
+
+# ----------------------------------------------------------------------------- model/taw_model.h
+def _nbytes(workspace, workspace_bytes):
+    if workspace_bytes is not None:
+        return workspace_bytes
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def _index_type(ids, given) -> int:
+    """TAW_I32 or TAW_I64 of a tensor of token ids or labels, which has to be dense: read with another type it would be read past its end.
+    An address has the type that the caller names."""
+    import torch
+    if ids is None or isinstance(ids, int):
+        return TAW_I64 if given is None else given
+    if ids.dtype == torch.int64:
+        kind = TAW_I64
+    elif ids.dtype == torch.int32:
+        kind = TAW_I32
+    else:
+        raise TawError(TAW_ERR_DTYPE, "TAW_ERR_DTYPE", f"token ids and labels are int32 or int64, not {ids.dtype}")
+    if not ids.is_contiguous():
+        raise TawError(TAW_ERR_SHAPE, "TAW_ERR_SHAPE", "token ids and labels must be contiguous")
+    return kind
+
+
+def make_embed_desc(dtype, T, H, V, scale=1.0, flags=0, ld_table=0, ld_x=0) -> taw_embed_desc:
+    return taw_embed_desc(dtype, T, H, V, ld_table, ld_x, scale, flags)
+
+
+def taw_embed_fwd(desc, ids, table, x, stream=None, id_type=None):
+    _check(load().taw_embed_fwd(C.byref(desc), _p(ids), _index_type(ids, id_type), _p(table), _p(x), _stream(stream)))
+
+
+def taw_embed_bwd_workspace_bytes(desc) -> int:
+    return int(load().taw_embed_bwd_workspace_bytes(C.byref(desc)))
+
+
+def taw_embed_bwd(desc, ids, dx, G, workspace, workspace_bytes=None, stream=None, id_type=None):
+    _check(load().taw_embed_bwd(C.byref(desc), _p(ids), _index_type(ids, id_type), _p(dx), _p(G), _p(workspace), _nbytes(workspace, workspace_bytes),
+                                _stream(stream)))
+
+
+def make_loss_desc(dtype, T, V, grad_dtype=None, ld=0, ld_grad=0, V_pad=0, label_smoothing=0.0, z_loss=0.0, grad_scale=1.0,
+                   flags=TAW_LOSS_MEAN) -> taw_loss_desc:
+    return taw_loss_desc(dtype, dtype if grad_dtype is None else grad_dtype, T, V, V_pad, ld, ld_grad, label_smoothing, z_loss, grad_scale, flags)
+
+
+def taw_loss_workspace_bytes(desc) -> int:
+    return int(load().taw_loss_workspace_bytes(C.byref(desc)))
+
+
+def taw_loss_fwd(desc, logits, labels, loss, loss_rows, lse, workspace, workspace_bytes=None, stream=None, label_type=None):
+    _check(load().taw_loss_fwd(C.byref(desc), _p(logits), _p(labels), _index_type(labels, label_type), _p(loss), _p(loss_rows), _p(lse), _p(workspace),
+                               _nbytes(workspace, workspace_bytes), _stream(stream)))
+
+
+def taw_loss_fwd_bwd(desc, logits, labels, loss, loss_rows, lse, dlogits, workspace, workspace_bytes=None, stream=None, label_type=None):
+    _check(load().taw_loss_fwd_bwd(C.byref(desc), _p(logits), _p(labels), _index_type(labels, label_type), _p(loss), _p(loss_rows), _p(lse), _p(dlogits),
+                                   _p(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
+
+
+def taw_loss_bwd(desc, logits, labels, lse, dloss_rows, dlogits, stream=None, label_type=None):
+    _check(load().taw_loss_bwd(C.byref(desc), _p(logits), _p(labels), _index_type(labels, label_type), _p(lse), _p(dloss_rows), _p(dlogits),
+                               _stream(stream)))
+
+
+class TensorList:
+    """A list of tensors as the norm and the clipping take it: made once, kept with the gradients."""
+
+    def __init__(self, tensors):
+        import torch
+        kinds = {torch.float32: TAW_F32, torch.bfloat16: TAW_BF16}
+        self.tensors = list(tensors)
+        for t in self.tensors:
+            if t.dtype not in kinds:
+                raise TawError(TAW_ERR_DTYPE, "TAW_ERR_DTYPE", f"gradients are float32 or bfloat16, not {t.dtype}")
+            if not t.is_contiguous():
+                raise TawError(TAW_ERR_SHAPE, "TAW_ERR_SHAPE", "gradients must be contiguous")
+        self.array = (taw_tensor * max(1, len(self.tensors)))(*[taw_tensor(t.data_ptr(), t.numel(), kinds[t.dtype]) for t in self.tensors])
+        self.count = len(self.tensors)
+
+
+def make_tensor_list(tensors) -> TensorList:
+    return TensorList(tensors)
+
+
+class ClipState:
+    """taw_clip_state on the device, and its fields as 0-dimensional tensors."""
+
+    def __init__(self, device="cuda"):
+        import torch
+        self.buffer = torch.zeros(4, dtype=torch.float64, device=device)
+        self.sumsq = self.buffer[0]
+        self.norm, self.coef = self.buffer.view(torch.float32)[2], self.buffer.view(torch.float32)[3]
+        self.nonfinite = self.buffer.view(torch.int32)[4]
+
+    def data_ptr(self):
+        return self.buffer.data_ptr()
+
+
+def new_clip_state(device="cuda") -> ClipState:
+    return ClipState(device)
+
+
+def taw_grad_norm_workspace_bytes(tensors) -> int:
+    return int(load().taw_grad_norm_workspace_bytes(tensors.array, tensors.count))
+
+
+def taw_grad_norm(tensors, max_norm, grad_scale, state, workspace, workspace_bytes=None, stream=None):
+    _check(load().taw_grad_norm(tensors.array, tensors.count, max_norm, grad_scale, _p(state), _p(workspace), _nbytes(workspace, workspace_bytes),
+                                _stream(stream)))
+
+
+def taw_grad_sumsq(tensors, accumulate, state, workspace, workspace_bytes=None, stream=None):
+    _check(load().taw_grad_sumsq(tensors.array, tensors.count, int(accumulate), _p(state), _p(workspace), _nbytes(workspace, workspace_bytes),
+                                 _stream(stream)))
+
+
+def taw_clip_coef(state, max_norm, grad_scale=1.0, stream=None):
+    _check(load().taw_clip_coef(_p(state), max_norm, grad_scale, _stream(stream)))
+
+
+def taw_grad_clip(tensors, state, stream=None):
+    _check(load().taw_grad_clip(tensors.array, tensors.count, _p(state), _stream(stream)))
+
+
+def taw_optimizer_step_clipped(state, W_chunk, chunk_dtype, master, m, v, G_shard, n_elems, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8,
+                               weight_decay=0.0, grad_scale=1.0, zero_grad=False, stream=None):
+    d = taw_adamw_desc(lr, beta1, beta2, eps, weight_decay, grad_scale, step, int(zero_grad))
+    _check(load().taw_optimizer_step_clipped(C.byref(d), _p(state), _p(W_chunk), chunk_dtype, _p(master), _p(m), _p(v), _p(G_shard), n_elems,
+                                             _stream(stream)))
 
 
 # ----------------------------------------------------------------------------- taw_ops.h

@@ -15,7 +15,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libtaw.so")
-SOURCES = ["taw_api.hip", "taw_sched.hip", "kernels_bw.hip", "kernels_generic.hip", "gemm_mfma.hip", "attn_mfma.hip", "diag.hip"]
+SOURCES = ["taw_api.hip", "taw_sched.hip", "kernels_bw.hip", "kernels_generic.hip", "gemm_mfma.hip", "attn_mfma.hip", "diag.hip",
+           "model_api.hip", "embed.hip", "loss.hip", "clip.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -24,8 +25,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
 
 def _headers():
     inc = os.path.join(os.path.dirname(HERE), "include")
-    return [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")] + \
-           [os.path.join(inc, f) for f in os.listdir(inc) if f.endswith(".h")]
+    return [os.path.join(d, f) for d in (CSRC, inc, os.path.join(inc, "model")) for f in os.listdir(d) if f.endswith(".h")]
 
 
 def _compile(src: str, force: bool) -> str:

@@ -1,0 +1,179 @@
+// Global gradient norm over a list of tensors, and clipping by it.
+//   sumsq = sum g^2 (fp64);  norm = |s| sqrt(sumsq);  coef = min(1, max_norm / norm)
+// Bound by memory: the norm reads every gradient once, the scaling in place reads and writes it once more.
+#include <cmath>
+
+#include "dev_common.h"
+#include "taw_internal.h"
+
+namespace taw {
+
+// Tensors travel as kernel arguments, so a call copies nothing to the device and can be captured; a longer list takes several launches.
+constexpr int kListMax = 120;
+constexpr int kPiece = 16384;                 // elements of a tensor that a workgroup takes at a time
+struct TensorList {
+  void* data[kListMax];
+  unsigned long long n[kListMax];
+  unsigned first[kListMax + 1];               // piece number of the tensor's first piece
+  unsigned char bf16[kListMax];
+  int count;
+};
+
+__device__ __forceinline__ int tensor_of(const TensorList& l, unsigned piece) {
+  int lo = 0, hi = l.count - 1;               // the last tensor that starts at or before the piece
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (l.first[mid] <= piece) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ double wave_sum_f64(double x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+
+// sum over a workgroup of NW wavefronts, in wavefront order; thread 0 has it
+template <int NW>
+__device__ __forceinline__ double block_sum_f64(double x) {
+  __shared__ double red[NW];
+  x = wave_sum_f64(x);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+  __syncthreads();
+  double s = 0.0;
+  if (threadIdx.x == 0)
+    for (int w = 0; w < NW; ++w) s += red[w];
+  return s;
+}
+
+// =============================================================================== sum of squares
+// Squares and sums in fp64: an fp32 square overflows from 1.8e19 on, and the fp64 units keep up with memory.
+template <typename T>
+__device__ __forceinline__ double piece_sumsq(const T* __restrict__ p, int m) {
+  double s = 0.0;
+  for (int i = threadIdx.x; i < m; i += 256) {
+    const double v = (double)(float)p[i];
+    s = fma(v, v, s);
+  }
+  return s;
+}
+
+__global__ void __launch_bounds__(256) sumsq_kernel(const TensorList l, double* __restrict__ partials) {
+  double s = 0.0;
+  for (unsigned piece = blockIdx.x; piece < l.first[l.count]; piece += gridDim.x) {
+    const int t = tensor_of(l, piece);
+    const unsigned long long at = (unsigned long long)(piece - l.first[t]) * kPiece;
+    const int m = (int)(l.n[t] - at < kPiece ? l.n[t] - at : kPiece);
+    s += l.bf16[t] ? piece_sumsq((const bf16_t*)l.data[t] + at, m) : piece_sumsq((const float*)l.data[t] + at, m);
+  }
+  s = block_sum_f64<4>(s);
+  if (threadIdx.x == 0) partials[blockIdx.x] = s;
+}
+
+__device__ __forceinline__ void finish_clip(double sumsq, float max_norm, float grad_scale, taw_clip_state* state) {
+  const float norm = (float)(fabs((double)grad_scale) * sqrt(sumsq));
+  const bool fine = norm <= 3.402823466e38f;  // false for NaN too
+  state->norm = norm;
+  state->coef = !fine ? 0.f : norm > max_norm ? max_norm / norm : 1.f;
+  state->nonfinite = fine ? 0 : 1;
+}
+
+__global__ void __launch_bounds__(256) sumsq_finish_kernel(const double* __restrict__ partials, int np, int set, int finish, float max_norm, float grad_scale,
+                                                           taw_clip_state* __restrict__ state) {
+  double s = 0.0;
+  for (int i = threadIdx.x; i < np; i += 256) s += partials[i];
+  s = block_sum_f64<4>(s);
+  if (threadIdx.x == 0) {
+    if (!set) s += state->sumsq;
+    state->sumsq = s;
+    if (finish) finish_clip(s, max_norm, grad_scale, state);
+  }
+}
+
+__global__ void __launch_bounds__(64) clip_coef_kernel(float max_norm, float grad_scale, taw_clip_state* __restrict__ state) {
+  if (threadIdx.x == 0) finish_clip(state->sumsq, max_norm, grad_scale, state);
+}
+
+// =============================================================================== scaling in place
+template <typename T>
+__device__ __forceinline__ void piece_scale(T* __restrict__ p, int m, float c) {
+  for (int i = threadIdx.x; i < m; i += 256) p[i] = (T)((float)p[i] * c);
+}
+
+__global__ void __launch_bounds__(256) clip_kernel(const TensorList l, const taw_clip_state* __restrict__ state) {
+  const float c = state->coef;
+  if (c == 1.f || state->nonfinite) return;
+  for (unsigned piece = blockIdx.x; piece < l.first[l.count]; piece += gridDim.x) {
+    const int t = tensor_of(l, piece);
+    const unsigned long long at = (unsigned long long)(piece - l.first[t]) * kPiece;
+    const int m = (int)(l.n[t] - at < kPiece ? l.n[t] - at : kPiece);
+    if (l.bf16[t]) piece_scale((bf16_t*)l.data[t] + at, m, c);
+    else piece_scale((float*)l.data[t] + at, m, c);
+  }
+}
+
+// =============================================================================== launchers
+static inline int last_err() { return (int)hipGetLastError(); }
+
+constexpr unsigned kGridMax = 2048;
+// cuts the list into launches; f(list, grid) returns a status
+template <typename F>
+static int over_list(const taw_tensor* t, int count, F f) {
+  TensorList l;
+  int i = 0;
+  while (i < count) {
+    l.count = 0;
+    unsigned pieces = 0;
+    for (; i < count && l.count < kListMax; ++i) {
+      if (!t[i].n) continue;
+      const unsigned long long np = (t[i].n + kPiece - 1) / kPiece;
+      if (np > 0x7fffffffull) return (int)hipErrorInvalidValue;
+      if (pieces + np > 0x7fffffffull) break;
+      l.data[l.count] = t[i].data;
+      l.n[l.count] = t[i].n;
+      l.bf16[l.count] = t[i].dtype == DT_BF16;
+      l.first[l.count++] = pieces;
+      pieces += (unsigned)np;
+    }
+    if (!pieces) continue;
+    l.first[l.count] = pieces;
+    const int e = f(l, pieces < kGridMax ? pieces : kGridMax);
+    if (e) return e;
+  }
+  return 0;
+}
+
+size_t grad_norm_workspace_bytes(const taw_tensor* t, int count) {
+  size_t blocks = 0;
+  over_list(t, count, [&](const TensorList&, unsigned grid) { blocks += grid; return 0; });
+  return blocks * sizeof(double) + 16;
+}
+
+int launch_grad_sumsq(const taw_tensor* t, int count, int set, int finish, float max_norm, float grad_scale, taw_clip_state* state, void* ws, hipStream_t st) {
+  double* partials = (double*)ws;
+  int np = 0;
+  const int e = over_list(t, count, [&](const TensorList& l, unsigned grid) {
+    hipLaunchKernelGGL(sumsq_kernel, dim3(grid), dim3(256), 0, st, l, partials + np);
+    np += (int)grid;
+    return last_err();
+  });
+  if (e) return e;
+  hipLaunchKernelGGL(sumsq_finish_kernel, dim3(1), dim3(256), 0, st, partials, np, set, finish, max_norm, grad_scale, state);
+  return last_err();
+}
+
+int launch_clip_coef(float max_norm, float grad_scale, taw_clip_state* state, hipStream_t st) {
+  hipLaunchKernelGGL(clip_coef_kernel, dim3(1), dim3(64), 0, st, max_norm, grad_scale, state);
+  return last_err();
+}
+
+int launch_grad_clip(const taw_tensor* t, int count, const taw_clip_state* state, hipStream_t st) {
+  return over_list(t, count, [&](const TensorList& l, unsigned grid) {
+    hipLaunchKernelGGL(clip_kernel, dim3(grid), dim3(256), 0, st, l, state);
+    return last_err();
+  });
+}
+
+}  // namespace taw

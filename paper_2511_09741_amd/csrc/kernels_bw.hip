@@ -361,11 +361,12 @@ __global__ void __launch_bounds__(256) grad_accum_kernel(float* __restrict__ G, 
 // leaves G zeroed for the next mini-batch.  b1c = 1 - beta1^t, b2c = 1 - beta2^t come from the host.
 // STREAM (bf16): a chunk that the memory-side cache cannot hold is stored past the caches, and a workgroup takes one row instead of two.
 template <bool STREAM> constexpr int kAdamRowsOf = STREAM ? 1 : 2;
-template <typename TW, bool STREAM>
+// CLIP: the scale of the gradients is multiplied by the coefficient that the gradient norm left on the device.
+template <typename TW, bool STREAM, bool CLIP>
 __global__ void __launch_bounds__(256) adamw_kernel(TW* __restrict__ chunk, float* __restrict__ master, float* __restrict__ m,
                                                      float* __restrict__ v, float* __restrict__ G, size_t n, float lr, float beta1,
                                                      float beta2, float eps, float wd, float b1c, float b2c, float gscale,
-                                                     int zero_grad) {
+                                                     int zero_grad, const taw_clip_state* __restrict__ clip) {
   constexpr int kAdamRows = kAdamRowsOf<STREAM>;
   const size_t nvec = n / 4;
   // Which product of a sum is fused with it is written out, as the kernel has always had it (by type, and for the up to three elements behind the last
@@ -379,6 +380,18 @@ __global__ void __launch_bounds__(256) adamw_kernel(TW* __restrict__ chunk, floa
     const float mh = mm / b1c, vh = vv / b2c;
     w = __builtin_fmaf(-lr, __builtin_fmaf(wd, w, mh / (sqrtf(vh) + eps)), w);
   };
+  if constexpr (CLIP) {
+    if (clip->nonfinite) {                 // the step is skipped
+      if (!zero_grad) return;
+      for (int u = 0; u < kAdamRows; ++u) {
+        const size_t i = (size_t)blockIdx.x * (kAdamRows * 256) + threadIdx.x + u * 256;
+        if (i < nvec) *reinterpret_cast<f32x4_t*>(G + 4 * i) = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      }
+      if (blockIdx.x == 0 && threadIdx.x < (n & 3)) G[nvec * 4 + threadIdx.x] = 0.f;
+      return;
+    }
+    gscale *= clip->coef;
+  }
   // a workgroup takes kAdamRows consecutive rows of 256 x 16 bytes of each array, once (as grad_accum_kernel does)
   const size_t i0 = (size_t)blockIdx.x * (kAdamRows * 256) + threadIdx.x;
   f32x4_t g4[kAdamRows], m4[kAdamRows], v4[kAdamRows], w4[kAdamRows];
@@ -627,15 +640,15 @@ int launch_grad_accum(float* G, const void* g, int src_dtype, size_t n, float sc
   return last_err();
 }
 
-template <typename TW, bool STREAM>
+template <typename TW, bool STREAM, bool CLIP>
 static int launch_adamw_as(void* chunk, float* master, float* m, float* v, float* G, size_t n, float lr, float beta1, float beta2, float eps, float wd, float b1c,
-                           float b2c, float gscale, int zero_grad, hipStream_t st) {
+                           float b2c, float gscale, int zero_grad, const taw_clip_state* clip, hipStream_t st) {
   constexpr size_t per = kAdamRowsOf<STREAM> * 256;
   size_t want = (n / 4 + per - 1) / per;
   if (want == 0) want = 1;
   if (want > 0x7fffffffu) return (int)hipErrorInvalidValue;
-  hipLaunchKernelGGL((adamw_kernel<TW, STREAM>), dim3((unsigned)want), dim3(256), 0, st, (TW*)chunk, master, m, v, G, n, lr, beta1, beta2, eps, wd, b1c, b2c, gscale,
-                     zero_grad);
+  hipLaunchKernelGGL((adamw_kernel<TW, STREAM, CLIP>), dim3((unsigned)want), dim3(256), 0, st, (TW*)chunk, master, m, v, G, n, lr, beta1, beta2, eps, wd, b1c, b2c,
+                     gscale, zero_grad, clip);
   return last_err();
 }
 
@@ -645,10 +658,12 @@ static int launch_adamw_as(void* chunk, float* master, float* m, float* v, float
 // 763 MiB 2546 -> 2431.  fp32 chunks have next to nothing from it (256 MiB 375 -> 434, 286 MiB 495 -> 493, 381 MiB 654 -> 655, 572 MiB 999 -> 984).
 constexpr size_t kAdamStreamBytes = (size_t)272 << 20;
 int launch_adamw(int w_dtype, void* chunk, float* master, float* m, float* v, float* G, size_t n, float lr, float beta1, float beta2,
-                 float eps, float wd, float b1c, float b2c, float gscale, int zero_grad, hipStream_t st) {
+                 float eps, float wd, float b1c, float b2c, float gscale, int zero_grad, const taw_clip_state* clip, hipStream_t st) {
   if (n == 0) return 0;
-  const auto f = w_dtype != DT_BF16 ? launch_adamw_as<float, false> : 2 * n > kAdamStreamBytes ? launch_adamw_as<bf16_t, true> : launch_adamw_as<bf16_t, false>;
-  return f(chunk, master, m, v, G, n, lr, beta1, beta2, eps, wd, b1c, b2c, gscale, zero_grad, st);
+  const bool past = w_dtype == DT_BF16 && 2 * n > kAdamStreamBytes;
+  const auto f = clip ? (w_dtype != DT_BF16 ? launch_adamw_as<float, false, true> : past ? launch_adamw_as<bf16_t, true, true> : launch_adamw_as<bf16_t, false, true>)
+                      : (w_dtype != DT_BF16 ? launch_adamw_as<float, false, false> : past ? launch_adamw_as<bf16_t, true, false> : launch_adamw_as<bf16_t, false, false>);
+  return f(chunk, master, m, v, G, n, lr, beta1, beta2, eps, wd, b1c, b2c, gscale, zero_grad, clip, st);
 }
 
 int launch_stage_copy(void* dst, const void* src, size_t bytes, hipStream_t st) {

@@ -12,13 +12,14 @@
 #include "../../include/taw.h"
 #include "../../include/taw_ops.h"
 #include "taw_internal.h"
+#include "taw_status.h"
 
 using namespace taw;
 
 // ------------------------------------------------------------------------------ error reporting
 static thread_local char g_err[512] = "";
 
-static int fail(int code, const char* fmt, ...) {
+int taw::fail(int code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);
@@ -26,7 +27,7 @@ static int fail(int code, const char* fmt, ...) {
   return code;
 }
 
-static int hip_fail(int hip_code, const char* what) {
+int taw::hip_fail(int hip_code, const char* what) {
   return fail(TAW_ERR_HIP, "%s: %s", what, hipGetErrorString((hipError_t)hip_code));
 }
 
@@ -45,13 +46,6 @@ extern "C" const char* taw_status_string(int status) {
 }
 
 extern "C" const char* taw_last_error(void) { return g_err; }
-
-static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-static inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-#define TAW_REQUIRE_PTR(p) do { if (!(p)) return fail(TAW_ERR_NULL, "%s is NULL", #p); } while (0)
-#define TAW_REQUIRE_ALIGNED(p) do { if (!aligned16(p)) return fail(TAW_ERR_ALIGN, "%s is not 16-byte aligned", #p); } while (0)
-#define TAW_LAUNCH(call, what) do { int e_ = (call); if (e_) return hip_fail(e_, what); } while (0)
 
 // ------------------------------------------------------------------------------ descriptor
 static int check_desc(const taw_layer_desc* d) {
@@ -355,8 +349,9 @@ extern "C" int taw_grad_accum(float* G_dst, const void* g_src, int32_t src_dtype
   return TAW_OK;
 }
 
-extern "C" int taw_optimizer_step(const taw_adamw_desc* opt, void* W_chunk, int32_t chunk_dtype, float* master, float* m, float* v,
-                                  float* G_shard, size_t n_elems, void* stream) {
+// also the front end of taw_optimizer_step_clipped, which adds the clip state
+int taw::optimizer_step(const taw_adamw_desc* opt, const taw_clip_state* clip, void* W_chunk, int32_t chunk_dtype, float* master, float* m, float* v, float* G_shard,
+                        size_t n_elems, hipStream_t stream) {
   if (!opt) return fail(TAW_ERR_NULL, "opt is NULL");
   if (chunk_dtype != TAW_F32 && chunk_dtype != TAW_BF16) return fail(TAW_ERR_DTYPE, "chunk_dtype %d is neither TAW_F32 nor TAW_BF16", chunk_dtype);
   if (opt->step < 1) return fail(TAW_ERR_SHAPE, "step=%d must be >= 1", opt->step);
@@ -373,8 +368,13 @@ extern "C" int taw_optimizer_step(const taw_adamw_desc* opt, void* W_chunk, int3
       if (ptrs[a] < ptrs[b] + lens[b] && ptrs[b] < ptrs[a] + lens[a]) return fail(TAW_ERR_SHAPE, "optimizer arrays overlap");
   const double b1c = 1.0 - pow((double)opt->beta1, (double)opt->step), b2c = 1.0 - pow((double)opt->beta2, (double)opt->step);
   TAW_LAUNCH(launch_adamw(chunk_dtype, W_chunk, master, m, v, G_shard, n_elems, opt->lr, opt->beta1, opt->beta2, opt->eps, opt->weight_decay,
-                          (float)b1c, (float)b2c, opt->grad_scale, opt->zero_grad, (hipStream_t)stream), "adamw kernel");
+                          (float)b1c, (float)b2c, opt->grad_scale, opt->zero_grad, clip, stream), "adamw kernel");
   return TAW_OK;
+}
+
+extern "C" int taw_optimizer_step(const taw_adamw_desc* opt, void* W_chunk, int32_t chunk_dtype, float* master, float* m, float* v,
+                                  float* G_shard, size_t n_elems, void* stream) {
+  return optimizer_step(opt, nullptr, W_chunk, chunk_dtype, master, m, v, G_shard, n_elems, (hipStream_t)stream);
 }
 
 extern "C" int taw_weight_stage(void* dst_buf, const void* src_shard, size_t bytes, void* copy_stream, void* wait_event, void* ready_event) {

@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "../../include/model/taw_model.h"
+
 namespace taw {
 
 enum { DT_F32 = 0, DT_BF16 = 1 };
@@ -47,9 +49,10 @@ int launch_swiglu_bwd(int dtype, int64_t T, int I, const void* da, const void* g
                       hipStream_t st);
 int launch_grad_accum(float* G, const void* g, int src_dtype, size_t n, float scale, hipStream_t st);
 int launch_stage_copy(void* dst, const void* src, size_t bytes, hipStream_t st);
-// AdamW over n elements; chunk in w_dtype, everything else fp32; b1c = 1 - beta1^t, b2c = 1 - beta2^t
+// AdamW over n elements; chunk in w_dtype, everything else fp32; b1c = 1 - beta1^t, b2c = 1 - beta2^t.  clip (device taw_clip_state, or
+// nullptr): gscale is multiplied by its coef, and nothing but G is touched where it says that the norm is not finite
 int launch_adamw(int w_dtype, void* chunk, float* master, float* m, float* v, float* G, size_t n, float lr, float beta1, float beta2,
-                 float eps, float wd, float b1c, float b2c, float gscale, int zero_grad, hipStream_t st);
+                 float eps, float wd, float b1c, float b2c, float gscale, int zero_grad, const taw_clip_state* clip, hipStream_t st);
 // D[b, h, t] = sum_i do[t, h*d + i] * o[t, h*d + i]   (o, do are [B*S, ld_o] / [B*S, ld_do])
 int launch_attn_rowdot(int dtype, int B, int S, int nh, int d, const void* o, int64_t ld_o,
                        const void* dO, int64_t ld_do, float* D, hipStream_t st);
@@ -189,5 +192,34 @@ size_t attn_bwd_mfma_scratch_floats(int B, int S, int nh, int form);
 // (table [S, 64, 2] fp32 of cos, sin) and dq, dk come out as gradients of the unrotated q, k
 int launch_attn_bwd_mfma(int B, int S, int nh, const void* qkv, const void* o, const void* dO, const float* lse,
                          float* scratch, void* dqkv, const float* rope_table, int form, hipStream_t st);
+
+// ---- what stands around the layers (embed.hip, loss.hip, clip.hip) ------------------------------
+enum { IDX_I32 = 0, IDX_I64 = 1 };
+struct EmbedArgs {
+  int dtype, id_type, T, H, V;
+  int64_t ld_table, ld_x;
+  float scale;
+  int accumulate;
+};
+int launch_embed_fwd(const EmbedArgs& a, const void* ids, const void* table, void* x, hipStream_t st);
+size_t embed_bwd_workspace_bytes(int T, int H, int V);
+int launch_embed_bwd(const EmbedArgs& a, const void* ids, const void* dx, float* G, void* ws, hipStream_t st);
+
+struct LossArgs {
+  int dtype, grad_dtype, label_type, T, V, V_pad;
+  int64_t ld, ld_grad;
+  float eps, z, grad_scale;
+  int mean;
+};
+size_t loss_workspace_bytes(int T);
+// dlogits == nullptr: the loss alone.  rows, lse may be nullptr
+int launch_loss(const LossArgs& a, const void* logits, const void* labels, float* loss, float* rows, float* lse, void* dlogits, void* ws, hipStream_t st);
+int launch_loss_bwd(const LossArgs& a, const void* logits, const void* labels, const float* lse, const float* dloss, void* dlogits, hipStream_t st);
+
+size_t grad_norm_workspace_bytes(const taw_tensor* t, int count);
+// set: 1 overwrites sumsq, 0 adds to it; finish: also norm, coef and nonfinite
+int launch_grad_sumsq(const taw_tensor* t, int count, int set, int finish, float max_norm, float grad_scale, taw_clip_state* state, void* ws, hipStream_t st);
+int launch_clip_coef(float max_norm, float grad_scale, taw_clip_state* state, hipStream_t st);
+int launch_grad_clip(const taw_tensor* t, int count, const taw_clip_state* state, hipStream_t st);
 
 }  // namespace taw
