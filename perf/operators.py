@@ -200,6 +200,8 @@ def _handles(s):
                                        flags=taw.TAW_LOSS_MEAN if c["mean"] else 0)
         s["ws"] = buffer(taw.taw_loss_workspace_bytes(s["desc"]))
     else:
+        if c["op"] == "step" and c["dtype"] == "f32":
+            s["chunk"] = s["master"].clone()      # a buffer of its own also where the types are the same
         s["list"] = taw.make_tensor_list(s["grads"])
         s["state"] = taw.new_clip_state()
         s["ws"] = buffer(taw.taw_grad_norm_workspace_bytes(s["list"]))
