@@ -62,6 +62,28 @@ template <> struct Vec<bf16_t, 1> {
   __device__ __forceinline__ void pin() { asm volatile("" : "+v"(raw)); }
 };
 
+template <> struct Vec<float, 2> {
+  f32x2_t raw;
+  __device__ __forceinline__ void load(const float* p) { raw = *reinterpret_cast<const f32x2_t*>(p); }
+  __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<f32x2_t*>(p) = raw; }
+  __device__ __forceinline__ float get(int i) const { return raw[i]; }
+  __device__ __forceinline__ void set(int i, float x) { raw[i] = x; }
+};
+template <> struct Vec<bf16_t, 4> {
+  bf16x4_t raw;
+  __device__ __forceinline__ void load(const bf16_t* p) { raw = *reinterpret_cast<const bf16x4_t*>(p); }
+  __device__ __forceinline__ void store(bf16_t* p) const { *reinterpret_cast<bf16x4_t*>(p) = raw; }
+  __device__ __forceinline__ float get(int i) const { return (float)raw[i]; }
+  __device__ __forceinline__ void set(int i, float x) { raw[i] = (bf16_t)x; }
+};
+template <> struct Vec<bf16_t, 2> {
+  bf16x2_t raw;
+  __device__ __forceinline__ void load(const bf16_t* p) { raw = *reinterpret_cast<const bf16x2_t*>(p); }
+  __device__ __forceinline__ void store(bf16_t* p) const { *reinterpret_cast<bf16x2_t*>(p) = raw; }
+  __device__ __forceinline__ float get(int i) const { return (float)raw[i]; }
+  __device__ __forceinline__ void set(int i, float x) { raw[i] = (bf16_t)x; }
+};
+
 template <typename T> struct VecWidth;
 template <> struct VecWidth<float> { static constexpr int value = 4; };
 template <> struct VecWidth<bf16_t> { static constexpr int value = 8; };

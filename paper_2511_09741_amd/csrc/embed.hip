@@ -16,68 +16,341 @@ __device__ __forceinline__ int row_id(const TI* __restrict__ ids, int64_t t, int
 }
 
 // =============================================================================== forward
-// one workgroup per token
-template <typename T, typename TI>
-__global__ void __launch_bounds__(256) embed_fwd_kernel(const TI* __restrict__ ids, const T* __restrict__ table, T* __restrict__ x, int H, int V, int64_t ld_table,
+// A thread moves one vector of each of U consecutive tokens' rows: U loads in flight.
+template <typename T, int VW, int U, typename TI>
+__global__ void __launch_bounds__(256) embed_fwd_kernel(const TI* __restrict__ ids, const T* __restrict__ table, T* __restrict__ x, int T_, int H, int V, int64_t ld_table,
                                                         int64_t ld_x, float scale) {
-  const int64_t t = blockIdx.x;
-  const int v = row_id(ids, t, V);
-  const T* src = table + (int64_t)(v < 0 ? 0 : v) * ld_table;
-  T* dst = x + t * ld_x;
-  for (int i = threadIdx.x; i < H; i += 256) dst[i] = v < 0 ? (T)0.f : (T)((float)src[i] * scale);
+  const unsigned cpr = (unsigned)(H / VW);
+  const uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint64_t group = idx / cpr;
+  const int64_t t0 = (int64_t)group * U;
+  if (t0 >= T_) return;
+  const int col = (int)(idx - group * cpr) * VW;
+  int v[U];
+#pragma unroll
+  for (int k = 0; k < U; ++k) v[k] = t0 + k < T_ ? row_id(ids, t0 + k, V) : -1;
+  Vec<T, VW> r[U];
+#pragma unroll
+  for (int k = 0; k < U; ++k)
+    if (v[k] >= 0) r[k].load(table + (int64_t)v[k] * ld_table + col);
+#pragma unroll
+  for (int k = 0; k < U; ++k) {
+    if (t0 + k >= T_) break;
+    Vec<T, VW> o;
+#pragma unroll
+    for (int j = 0; j < VW; ++j) o.set(j, v[k] >= 0 ? r[k].get(j) * scale : 0.f);
+    o.store(x + (t0 + k) * ld_x + col);
+  }
 }
 
 // =============================================================================== backward
-// one workgroup per row of the table and 256 columns; it looks through all the ids, in order
-template <typename T, typename TI>
-__global__ void __launch_bounds__(256) embed_bwd_kernel(const TI* __restrict__ ids, const T* __restrict__ dx, float* __restrict__ G, int T_, int H, int V, int64_t ld_table,
-                                                        int64_t ld_x, float scale, int accumulate) {
-  const int v = blockIdx.x, col = blockIdx.y * 256 + threadIdx.x, lane = threadIdx.x & 63;
-  float s = 0.f;
-  bool any = false;
-  for (int t0 = 0; t0 < T_; t0 += 64) {
-    const bool mine = t0 + lane < T_ && row_id(ids, t0 + lane, V) == v;
-    unsigned long long who = __ballot(mine);
-    while (who) {
-      const int t = t0 + __builtin_ctzll(who);
-      who &= who - 1;
-      any = true;
-      if (col < H) s += (float)dx[(int64_t)t * ld_x + col];
+// The tokens are sorted by id (stable: tokens of one id keep their order), then the sorted sequence is cut into pieces of K tokens, and the rows of
+// dx of a piece are summed id by id.  An id with at most K tokens is summed whole, by the piece it starts in (which so reads up to K - 1 tokens
+// beyond its end); one with more leaves a partial sum in every piece it has a part in, and a last kernel adds those up in order.  So no thread reads
+// more than 2 K rows whatever the ids are, every row of dx is read once, and the result does not depend on scheduling.
+
+constexpr int kSortWaves = 16;
+constexpr int kSortMaxRange = 1024;            // ids that a workgroup of the sort owns at most
+
+// Workgroup w owns the ids [w R, (w + 1) R).  It goes through all the tokens twice: to count its own ids by wavefront (each has a contiguous run of
+// tokens) and the tokens with smaller ids, which is where its part of the sorted sequence starts; and to place its own.  No workgroup waits for
+// another, nothing is cleared beforehand.  The ids are read from L2 (256 times 128 KiB at 32768 tokens).
+// perm: token at a sorted place; sid: its id; start[v], start[V]: where the tokens of v start, and the number of tokens that name a row.
+template <typename TI>
+__global__ void __launch_bounds__(1024) embed_sort_kernel(const TI* __restrict__ ids, int T_, int V, int R, int* __restrict__ perm, int* __restrict__ sid,
+                                                          int* __restrict__ start) {
+  extern __shared__ int cnt[];                 // [kSortWaves][R]
+  __shared__ int wsum[kSortWaves], lsum[kSortWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int v0 = blockIdx.x * R, v1 = v0 + R < V ? v0 + R : V;
+  for (int i = threadIdx.x; i < kSortWaves * R; i += 1024) cnt[i] = 0;
+  __syncthreads();
+  const int run = ((T_ + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
+  const int t0 = wave * run, t1 = t0 + run < T_ ? t0 + run : T_;
+  int* mycnt = cnt + wave * R;
+  int less = 0;
+  constexpr int U = 8;
+  for (int t = t0; t < t1; t += 64 * U) {
+    int v[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) v[k] = t + 64 * k + lane < t1 ? row_id(ids, t + 64 * k + lane, V) : -1;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      less += v[k] >= 0 && v[k] < v0;
+      const bool mine = v[k] >= v0 && v[k] < v1;
+      unsigned long long left = __ballot(mine);
+      while (left) {                           // one turn for each different id of the 64
+        const int f = __builtin_ctzll(left);
+        const int id = __shfl(v[k], f, 64);
+        const unsigned long long same = __ballot(mine && v[k] == id);
+        if (lane == f) mycnt[id - v0] += __popcll(same);
+        left &= ~same;
+      }
     }
   }
-  if (col >= H) return;
-  float* g = G + (int64_t)v * ld_table + col;
-  if (!accumulate) *g = scale * s;
-  else if (any) *g += scale * s;
+  for (int o = 32; o > 0; o >>= 1) less += __shfl_xor(less, o, 64);
+  if (lane == 0) lsum[wave] = less;
+  __syncthreads();
+  // where each id's tokens start, and within them each wavefront's
+  int total = 0;
+  const int r = threadIdx.x;                   // R <= 1024
+  if (r < R)
+    for (int w = 0; w < kSortWaves; ++w) total += cnt[w * R + r];
+  int incl = total;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int up = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += up;
+  }
+  if (lane == 63) wsum[wave] = incl;
+  __syncthreads();
+  int at = incl - total;
+  for (int w = 0; w < kSortWaves; ++w) {
+    at += lsum[w];
+    if (w < wave) at += wsum[w];
+  }
+  if (r < R && v0 + r < V) {
+    start[v0 + r] = at;
+    int off = at;
+    for (int w = 0; w < kSortWaves; ++w) {
+      const int c = cnt[w * R + r];
+      cnt[w * R + r] = off;
+      off += c;
+    }
+    if (v0 + r == V - 1) start[V] = off;
+  }
+  __syncthreads();
+  for (int t = t0; t < t1; t += 64 * U) {
+    int v[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) v[k] = t + 64 * k + lane < t1 ? row_id(ids, t + 64 * k + lane, V) : -1;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const bool mine = v[k] >= v0 && v[k] < v1;
+      unsigned long long left = __ballot(mine);
+      while (left) {
+        const int f = __builtin_ctzll(left);
+        const int id = __shfl(v[k], f, 64);
+        const unsigned long long same = __ballot(mine && v[k] == id);
+        const int base = mycnt[id - v0];
+        if (mine && v[k] == id) {
+          const int pos = base + __popcll(same & ((1ull << lane) - 1));
+          perm[pos] = t + 64 * k + lane;
+          sid[pos] = id;
+        }
+        if (lane == f) mycnt[id - v0] = base + __popcll(same);
+        left &= ~same;
+      }
+    }
+  }
+}
+
+// sums of pieces: a thread has one vector of columns of a piece.  part: [pieces][2][H]: the sum of the long id that a piece starts within (0), and of
+// the one that starts in it and goes on behind it (1).  The threads behind those of the pieces zero the rows that no token names.
+template <typename T, int VW>
+__global__ void __launch_bounds__(256) embed_rows_kernel(const int* __restrict__ perm, const int* __restrict__ sid, const int* __restrict__ start, const T* __restrict__ dx,
+                                                         float* __restrict__ G, float* __restrict__ part, int H, int V, int64_t ld_table, int64_t ld_x, float scale,
+                                                         int accumulate, int K, unsigned piece_blocks) {
+  constexpr int U = 8;
+  const unsigned cpr = (unsigned)(H / VW);
+  typedef float fv_t __attribute__((ext_vector_type(VW), aligned(VW * 4 < 16 ? VW * 4 : 16)));
+  if (blockIdx.x >= piece_blocks) {
+    const uint64_t idx = (uint64_t)(blockIdx.x - piece_blocks) * 256 + threadIdx.x;
+    const uint64_t q = idx / cpr;
+    const int col = (int)(idx - q * cpr) * VW;
+    for (int k = 0; k < 4; ++k) {
+      const int64_t v = (int64_t)q * 4 + k;
+      if (v < V && start[v] == start[v + 1]) *reinterpret_cast<fv_t*>(G + v * ld_table + col) = fv_t(0.f);
+    }
+    return;
+  }
+  const uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint64_t p = idx / cpr;
+  const int col = (int)(idx - p * cpr) * VW;
+  const int n = start[V];
+  if (p * K >= (uint64_t)n) return;
+  const int p0 = (int)p * K, p1 = p0 + K < n ? p0 + K : n;
+  int from = p0, to = p1;
+  bool head = false, tail = false;
+  {
+    const int v = sid[p0], s = start[v], e = start[v + 1];
+    if (s < p0) {
+      head = e - s > K;
+      if (!head) from = e;                     // its start's piece has it whole
+    }
+  }
+  {
+    const int v = sid[p1 - 1], s = start[v], e = start[v + 1];
+    if (e > p1) {
+      tail = e - s > K;
+      if (!tail) to = e;
+    }
+  }
+  if (from >= to) return;
+  fv_t acc = fv_t(0.f);
+  int cur = sid[from];
+  auto flush = [&](bool last) {
+    if (head || (last && tail)) {
+      *reinterpret_cast<fv_t*>(part + ((int64_t)p * 2 + (head ? 0 : 1)) * H + col) = acc;
+    } else {
+      float* g = G + (int64_t)cur * ld_table + col;
+      fv_t o = acc * scale;
+      if (accumulate) o += *reinterpret_cast<const fv_t*>(g);
+      *reinterpret_cast<fv_t*>(g) = o;
+    }
+    head = false;
+  };
+  for (int q = from; q < to; q += U) {
+    int who[U], id[U];
+    Vec<T, VW> r[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int at = q + k < to ? q + k : to - 1;
+      who[k] = perm[at];
+      id[k] = sid[at];
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k) r[k].load(dx + (int64_t)who[k] * ld_x + col);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (q + k >= to) break;
+      if (id[k] != cur) {
+        flush(false);
+        cur = id[k];
+        acc = fv_t(0.f);
+      }
+#pragma unroll
+      for (int j = 0; j < VW; ++j) acc[j] += r[k].get(j);
+    }
+  }
+  flush(true);
+}
+
+// The ids with more than K tokens: the workgroups of the piece that such an id starts in add up its partial sums, wavefront w those of the pieces
+// w, w + 4, ... counted from there, then the four in order.
+__global__ void __launch_bounds__(256) embed_join_kernel(const int* __restrict__ sid, const int* __restrict__ start, const float* __restrict__ part, float* __restrict__ G,
+                                                         int H, int V, int64_t ld_table, float scale, int accumulate, int K) {
+  __shared__ float red[4][64];
+  const int n = start[V];
+  const int64_t p = blockIdx.x;
+  if ((p + 1) * K >= n) return;
+  const int v = sid[(p + 1) * K - 1], s = start[v], e = start[v + 1];
+  if (s < p * K || e <= (p + 1) * K || e - s <= K) return;
+  const int np = (int)((e - 1) / K - p) + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int c0 = blockIdx.y * 64; c0 < H; c0 += gridDim.y * 64) {
+    const int col = c0 + lane;
+    float t = 0.f;
+    if (col < H) {
+#pragma unroll 8
+      for (int k = wave; k < np; k += 4) t += part[((p + k) * 2 + (k ? 0 : 1)) * H + col];
+    }
+    red[wave][lane] = t;
+    __syncthreads();
+    if (wave == 0 && col < H) {
+      t = scale * (((red[0][lane] + red[1][lane]) + red[2][lane]) + red[3][lane]);
+      float* g = G + (int64_t)v * ld_table + col;
+      *g = accumulate ? *g + t : t;
+    }
+    __syncthreads();
+  }
 }
 
 // =============================================================================== launchers
 static inline int last_err() { return (int)hipGetLastError(); }
 
+// the widest vector of 1, 2, 4 (8 for bf16) elements that the row length and the strides are multiples of
+static int width_of(int dtype, int64_t a, int64_t b, int64_t c) {
+  const int64_t m = a | b | c;
+  return m % 8 == 0 && dtype == DT_BF16 ? 8 : m % 4 == 0 ? 4 : m % 2 == 0 ? 2 : 1;
+}
+
+template <int VW> using width_t = std::integral_constant<int, VW>;
 template <typename F>
-static int by_types(int dtype, int id_type, F f) {
-  if (dtype == DT_BF16) return id_type == IDX_I64 ? f((bf16_t*)nullptr, (int64_t*)nullptr) : f((bf16_t*)nullptr, (int32_t*)nullptr);
-  return id_type == IDX_I64 ? f((float*)nullptr, (int64_t*)nullptr) : f((float*)nullptr, (int32_t*)nullptr);
+static int by_types(const EmbedArgs& a, F f) {
+  const int w = width_of(a.dtype, a.H, a.ld_table, a.ld_x);
+  const auto sized = [&](auto* t, auto* i) {
+    using T = std::remove_pointer_t<decltype(t)>;
+    if constexpr (sizeof(T) == 2)
+      if (w == 8) return f(t, i, width_t<8>{});
+    return w == 4 ? f(t, i, width_t<4>{}) : w == 2 ? f(t, i, width_t<2>{}) : f(t, i, width_t<1>{});
+  };
+  if (a.dtype == DT_BF16) return a.id_type == IDX_I64 ? sized((bf16_t*)nullptr, (int64_t*)nullptr) : sized((bf16_t*)nullptr, (int32_t*)nullptr);
+  return a.id_type == IDX_I64 ? sized((float*)nullptr, (int64_t*)nullptr) : sized((float*)nullptr, (int32_t*)nullptr);
+}
+
+static bool grid_of(uint64_t threads, uint64_t* blocks) {
+  *blocks = (threads + 255) / 256;
+  return *blocks <= 0x7fffffffu;
 }
 
 int launch_embed_fwd(const EmbedArgs& a, const void* ids, const void* table, void* x, hipStream_t st) {
-  return by_types(a.dtype, a.id_type, [&](auto* t, auto* i) {
+  return by_types(a, [&](auto* t, auto* i, auto w) {
     using T = std::remove_pointer_t<decltype(t)>;
     using TI = std::remove_pointer_t<decltype(i)>;
-    hipLaunchKernelGGL((embed_fwd_kernel<T, TI>), dim3((unsigned)a.T), dim3(256), 0, st, (const TI*)ids, (const T*)table, (T*)x, a.H, a.V, a.ld_table, a.ld_x, a.scale);
+    constexpr int VW = decltype(w)::value, U = 4;
+    uint64_t blocks;
+    if (!grid_of((uint64_t)((a.T + U - 1) / U) * (a.H / VW), &blocks)) return (int)hipErrorInvalidValue;
+    hipLaunchKernelGGL((embed_fwd_kernel<T, VW, U, TI>), dim3((unsigned)blocks), dim3(256), 0, st, (const TI*)ids, (const T*)table, (T*)x, a.T, a.H, a.V, a.ld_table, a.ld_x,
+                       a.scale);
     return last_err();
   });
 }
 
-size_t embed_bwd_workspace_bytes(int, int, int) { return 0; }
+// tokens of a piece
+static int piece_of(int) { return 32; }
 
-int launch_embed_bwd(const EmbedArgs& a, const void* ids, const void* dx, float* G, void*, hipStream_t st) {
-  return by_types(a.dtype, a.id_type, [&](auto* t, auto* i) {
+struct EmbedWork {
+  int *perm, *sid, *start;
+  float* part;
+  size_t bytes;
+};
+static EmbedWork embed_work(int T_, int H, int V, void* base) {
+  size_t off = 0;
+  const auto take = [&](size_t bytes) {
+    char* p = (char*)base + off;
+    off += (bytes + 255) / 256 * 256;
+    return (void*)p;
+  };
+  EmbedWork w;
+  w.perm = (int*)take((size_t)T_ * 4);
+  w.sid = (int*)take((size_t)T_ * 4);
+  w.start = (int*)take(((size_t)V + 1) * 4);
+  const size_t K = piece_of(T_), pieces = (T_ + K - 1) / K;
+  w.part = (float*)take(T_ > (int)K ? pieces * 2 * H * 4 : 0);
+  w.bytes = off;
+  return w;
+}
+
+size_t embed_bwd_workspace_bytes(int T_, int H, int V) { return embed_work(T_, H, V, nullptr).bytes; }
+
+int launch_embed_bwd(const EmbedArgs& a, const void* ids, const void* dx, float* G, void* ws, hipStream_t st) {
+  return by_types(a, [&](auto* t, auto* i, auto w) {
     using T = std::remove_pointer_t<decltype(t)>;
     using TI = std::remove_pointer_t<decltype(i)>;
-    hipLaunchKernelGGL((embed_bwd_kernel<T, TI>), dim3((unsigned)a.V, (unsigned)((a.H + 255) / 256)), dim3(256), 0, st, (const TI*)ids, (const T*)dx, G, a.T, a.H, a.V,
-                       a.ld_table, a.ld_x, a.scale, a.accumulate);
-    return last_err();
+    constexpr int VW = decltype(w)::value;
+    const EmbedWork k = embed_work(a.T, a.H, a.V, ws);
+    const int K = piece_of(a.T);
+    const int per = (a.V + 255) / 256, R = per < kSortMaxRange ? per : kSortMaxRange;
+    TAW_SET_LDS_LIMIT_ONCE((embed_sort_kernel<TI>), kSortWaves * kSortMaxRange * sizeof(int));
+    hipLaunchKernelGGL((embed_sort_kernel<TI>), dim3((unsigned)((a.V + R - 1) / R)), dim3(1024), kSortWaves * R * sizeof(int), st, (const TI*)ids, a.T, a.V, R, k.perm, k.sid,
+                       k.start);
+    int e = last_err();
+    if (e) return e;
+    const uint64_t cpr = a.H / VW, pieces = (a.T + K - 1) / K;
+    uint64_t pb, zb;
+    if (!grid_of(pieces * cpr, &pb) || !grid_of(a.accumulate ? 0 : (uint64_t)((a.V + 3) / 4) * cpr, &zb) || pb + zb > 0x7fffffffu) return (int)hipErrorInvalidValue;
+    if (pb + zb) {
+      hipLaunchKernelGGL((embed_rows_kernel<T, VW>), dim3((unsigned)(pb + zb)), dim3(256), 0, st, k.perm, k.sid, k.start, (const T*)dx, G, k.part, a.H, a.V, a.ld_table, a.ld_x,
+                         a.scale, a.accumulate, K, (unsigned)pb);
+      e = last_err();
+      if (e) return e;
+    }
+    if (pieces > 1) {
+      const unsigned cols = (unsigned)((a.H + 63) / 64);
+      hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)pieces, cols < 16 ? cols : 16), dim3(256), 0, st, k.sid, k.start, k.part, G, a.H, a.V, a.ld_table, a.scale, a.accumulate,
+                         K);
+      e = last_err();
+    }
+    return e;
   });
 }
 
