@@ -59,7 +59,7 @@ extern "C" int taw_embed_fwd(const taw_embed_desc* desc, const void* ids, int32_
 
 extern "C" size_t taw_embed_bwd_workspace_bytes(const taw_embed_desc* desc) {
   EmbedArgs a;
-  return check_embed(desc, &a) ? 0 : embed_bwd_workspace_bytes(a.T, a.H, a.V);
+  return check_embed(desc, &a) ? 0 : embed_bwd_workspace_bytes(a);
 }
 
 extern "C" int taw_embed_bwd(const taw_embed_desc* desc, const void* ids, int32_t id_type, const void* dx, float* G, void* workspace,
@@ -76,7 +76,7 @@ extern "C" int taw_embed_bwd(const taw_embed_desc* desc, const void* ids, int32_
     TAW_REQUIRE_ALIGNED(dx);
   }
   TAW_REQUIRE_PTR(G); TAW_REQUIRE_ALIGNED(G);
-  const size_t need = embed_bwd_workspace_bytes(a.T, a.H, a.V);
+  const size_t need = embed_bwd_workspace_bytes(a);
   if (workspace_bytes < need) return fail(TAW_ERR_WORKSPACE, "workspace_bytes=%zu < required %zu", workspace_bytes, need);
   if (need) { TAW_REQUIRE_PTR(workspace); TAW_REQUIRE_ALIGNED(workspace); }
   const size_t nG = span(a.V, a.H, a.ld_table, 4), nd = span(a.T, a.H, a.ld_x, dt_size(a.dtype)), ni = (size_t)a.T * (id_type == TAW_I64 ? 8 : 4);

@@ -202,7 +202,7 @@ struct EmbedArgs {
   int accumulate;
 };
 int launch_embed_fwd(const EmbedArgs& a, const void* ids, const void* table, void* x, hipStream_t st);
-size_t embed_bwd_workspace_bytes(int T, int H, int V);
+size_t embed_bwd_workspace_bytes(const EmbedArgs& a);
 int launch_embed_bwd(const EmbedArgs& a, const void* ids, const void* dx, float* G, void* ws, hipStream_t st);
 
 struct LossArgs {
