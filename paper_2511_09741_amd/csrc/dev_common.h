@@ -65,6 +65,7 @@ template <> struct Vec<bf16_t, 1> {
 template <> struct Vec<float, 2> {
   f32x2_t raw;
   __device__ __forceinline__ void load(const float* p) { raw = *reinterpret_cast<const f32x2_t*>(p); }
+  __device__ __forceinline__ void load_nt(const float* p) { raw = __builtin_nontemporal_load(reinterpret_cast<const f32x2_t*>(p)); }
   __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<f32x2_t*>(p) = raw; }
   __device__ __forceinline__ void store_nt(float* p) const { __builtin_nontemporal_store(raw, reinterpret_cast<f32x2_t*>(p)); }
   __device__ __forceinline__ float get(int i) const { return raw[i]; }
@@ -73,6 +74,7 @@ template <> struct Vec<float, 2> {
 template <> struct Vec<bf16_t, 4> {
   bf16x4_t raw;
   __device__ __forceinline__ void load(const bf16_t* p) { raw = *reinterpret_cast<const bf16x4_t*>(p); }
+  __device__ __forceinline__ void load_nt(const bf16_t* p) { raw = __builtin_nontemporal_load(reinterpret_cast<const bf16x4_t*>(p)); }
   __device__ __forceinline__ void store(bf16_t* p) const { *reinterpret_cast<bf16x4_t*>(p) = raw; }
   __device__ __forceinline__ void store_nt(bf16_t* p) const { __builtin_nontemporal_store(raw, reinterpret_cast<bf16x4_t*>(p)); }
   __device__ __forceinline__ float get(int i) const { return (float)raw[i]; }
@@ -81,6 +83,7 @@ template <> struct Vec<bf16_t, 4> {
 template <> struct Vec<bf16_t, 2> {
   bf16x2_t raw;
   __device__ __forceinline__ void load(const bf16_t* p) { raw = *reinterpret_cast<const bf16x2_t*>(p); }
+  __device__ __forceinline__ void load_nt(const bf16_t* p) { raw = __builtin_nontemporal_load(reinterpret_cast<const bf16x2_t*>(p)); }
   __device__ __forceinline__ void store(bf16_t* p) const { *reinterpret_cast<bf16x2_t*>(p) = raw; }
   __device__ __forceinline__ void store_nt(bf16_t* p) const { __builtin_nontemporal_store(raw, reinterpret_cast<bf16x2_t*>(p)); }
   __device__ __forceinline__ float get(int i) const { return (float)raw[i]; }

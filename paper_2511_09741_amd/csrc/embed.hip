@@ -69,22 +69,25 @@ static SortShape sort_shape(int V) {
   return s;
 }
 
-// A workgroup goes through all the tokens twice: to count its own ids by wavefront (each has a contiguous run of tokens) and the tokens of the
-// workgroups before it, which is where its part of the sorted sequence starts; and to place its own.  No workgroup waits for another, nothing is
-// cleared beforehand.  The ids are read from L2 (256 times 128 KiB at 32768 tokens).
+// A workgroup goes through all the tokens to count its own ids by wavefront (each has a contiguous run of tokens) and the tokens of the workgroups
+// before it, which is where its part of the sorted sequence starts; then it places its own, which the wavefronts have listed in LDS (one that found
+// more than kSortList goes through its run again).  No workgroup waits for another, nothing is cleared beforehand.  The ids are read from L2 (256 times
+// 128 KiB at 32768 tokens).  Bound by latency, so it also zeroes the rows of G that no token names, whose stores nobody waits for.
 // perm: token at a sorted place; sid: its id; start[place_of(v)], start[own nb]: where the tokens of v start, and the number of tokens that name a row.
+constexpr int kSortList = 512;
+constexpr int kRunBits = 20;                   // T <= 2^24: a run has at most 2^20 tokens, and an id is one of 2^10 of its workgroup
 template <typename TI>
 __global__ void __launch_bounds__(1024) embed_sort_kernel(const TI* __restrict__ ids, int T_, int V, SortShape sh, int* __restrict__ perm, int* __restrict__ sid,
-                                                          int* __restrict__ start) {
+                                                          int* __restrict__ start, float* __restrict__ G, int H, int64_t ld_table) {
   extern __shared__ int cnt[];                 // [kSortWaves][own]
-  __shared__ int wsum[kSortWaves], lsum[kSortWaves];
+  __shared__ int list[kSortWaves][kSortList], totals[kSortMaxOwn], wsum[kSortWaves], lsum[kSortWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, R = sh.own, w0 = blockIdx.x;
   for (int i = threadIdx.x; i < kSortWaves * R; i += 1024) cnt[i] = 0;
   __syncthreads();
   const int run = ((T_ + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
   const int t0 = wave * run, t1 = t0 + run < T_ ? t0 + run : T_;
   int* mycnt = cnt + wave * R;
-  int less = 0;
+  int less = 0, found = 0;
   constexpr int U = 16;
   for (int t = t0; t < t1; t += 64 * U) {
     int v[U];
@@ -98,7 +101,14 @@ __global__ void __launch_bounds__(1024) embed_sort_kernel(const TI* __restrict__
     for (int k = 0; k < U; ++k) {
       const int g = v[k] < 0 ? 0x7fffffff : sh.group_of(v[k]);
       less += g < w0;
-      if (g == w0) atomicAdd(&mycnt[v[k] >> sh.lb], 1);
+      const unsigned long long mine = __ballot(g == w0);
+      if (!mine) continue;
+      if (g == w0) {
+        const int r = v[k] >> sh.lb, at = found + __popcll(mine & ((1ull << lane) - 1));
+        atomicAdd(&mycnt[r], 1);
+        if (at < kSortList) list[wave][at] = (r << kRunBits) | (t - t0 + 64 * k + lane);
+      }
+      found += __popcll(mine);
     }
   }
   for (int o = 32; o > 0; o >>= 1) less += __shfl_xor(less, o, 64);
@@ -107,8 +117,10 @@ __global__ void __launch_bounds__(1024) embed_sort_kernel(const TI* __restrict__
   // where each id's tokens start, and within them each wavefront's
   int total = 0;
   const int r = threadIdx.x;                   // R <= 1024
-  if (r < R)
+  if (r < R) {
     for (int w = 0; w < kSortWaves; ++w) total += cnt[w * R + r];
+    totals[r] = total;
+  }
   int incl = total;
   for (int o = 1; o < 64; o <<= 1) {
     const int up = __shfl_up(incl, o, 64);
@@ -132,61 +144,58 @@ __global__ void __launch_bounds__(1024) embed_sort_kernel(const TI* __restrict__
     if (r == R - 1 && w0 == (int)gridDim.x - 1) start[w0 * R + R] = off;
   }
   __syncthreads();
-  for (int t = t0; t < t1; t += 64 * U) {
-    int v[U];
-#pragma unroll
-    for (int k = 0; k < U; ++k) {                // all the loads first, whatever lies behind the run
-      const int at = t + 64 * k + lane;
-      v[k] = row_id(ids, at < t1 ? at : t1 - 1, V);
-      if (at >= t1) v[k] = -1;
-    }
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-      const bool mine = v[k] >= 0 && sh.group_of(v[k]) == w0;
-      unsigned long long left = __ballot(mine);
-      while (left) {                           // one turn for each different id of the 64: mostly none or one
-        const int f = __builtin_ctzll(left);
-        const int id = __builtin_amdgcn_readlane(v[k], f);
-        const unsigned long long same = __ballot(mine && v[k] == id);
-        const int base = mycnt[id >> sh.lb];
-        if (mine && v[k] == id) {
-          const int pos = base + __popcll(same & ((1ull << lane) - 1));
-          perm[pos] = t + 64 * k + lane;
-          sid[pos] = id;
-        }
-        if (lane == f) mycnt[id >> sh.lb] = base + __popcll(same);
-        left &= ~same;
+  // places 64 tokens of the run, in order: one turn for each different id among them
+  auto place = [&](bool mine, int own, int token) {
+    unsigned long long left = __ballot(mine);
+    while (left) {
+      const int f = __builtin_ctzll(left);
+      const int id = __builtin_amdgcn_readlane(own, f);
+      const unsigned long long same = __ballot(mine && own == id);
+      const int base = mycnt[id];
+      if (mine && own == id) {
+        const int pos = base + __popcll(same & ((1ull << lane) - 1));
+        perm[pos] = token;
+        sid[pos] = (id << sh.lb) | ((w0 - id) & ((1 << sh.lb) - 1));
       }
+      if (lane == f) mycnt[id] = base + __popcll(same);
+      left &= ~same;
     }
+  };
+  if (found <= kSortList) {
+    for (int i = 0; i < found; i += 64) {
+      const int e = i + lane < found ? list[wave][i + lane] : 0;
+      place(i + lane < found, e >> kRunBits, t0 + (e & ((1 << kRunBits) - 1)));
+    }
+  } else {
+    for (int t = t0; t < t1; t += 64) {
+      const int v = t + lane < t1 ? row_id(ids, t + lane, V) : -1;
+      place(v >= 0 && sh.group_of(v) == w0, v >> sh.lb, t + lane);
+    }
+  }
+  if (!G) return;
+  const bool wide = ((H | ld_table) & 3) == 0;
+  for (int own = wave; own < R; own += kSortWaves) {
+    const int v = (own << sh.lb) | ((w0 - own) & ((1 << sh.lb) - 1));
+    if (totals[own] || v >= V) continue;
+    float* g = G + (int64_t)v * ld_table;
+    if (wide)
+      for (int c = 4 * lane; c < H; c += 256) __builtin_nontemporal_store(f32x4_t{0.f, 0.f, 0.f, 0.f}, reinterpret_cast<f32x4_t*>(g + c));
+    else
+      for (int c = lane; c < H; c += 64) g[c] = 0.f;
   }
 }
 
 // Sums of pieces: a thread has one vector of columns of a piece.  part: [pieces][2][H]: the sum of the long id that a piece starts within (0), and of
-// the one that starts in it and goes on behind it (1).  The threads behind those of the pieces zero the rows that no token names.
-constexpr int kZeroRows = 4;
-template <typename T, int VW>
+// the one that starts in it and goes on behind it (1).
+// Four columns a thread, also of bf16: the sums are stored 16 bytes a lane side by side (32768 tokens of 4096 into 32000 rows: 185 us with four, 192 with
+// eight).  STREAM: dx and G go past L2 (180 us; 4503 tokens of 1024, which L2 has room for: 24.8 against 23.3).
+template <typename T, int VW, bool STREAM>
 __global__ void __launch_bounds__(256) embed_rows_kernel(const int* __restrict__ perm, const int* __restrict__ sid, const int* __restrict__ start, const T* __restrict__ dx,
-                                                         float* __restrict__ G, float* __restrict__ part, int H, int V, SortShape sh, int64_t ld_table, int64_t ld_x,
-                                                         float scale, int accumulate, int K, unsigned piece_blocks) {
+                                                         float* __restrict__ G, float* __restrict__ part, int H, SortShape sh, int64_t ld_table, int64_t ld_x,
+                                                         float scale, int accumulate, int K) {
   constexpr int U = 8;
   const unsigned cpr = (unsigned)(H / VW);
   typedef float fv_t __attribute__((ext_vector_type(VW), aligned(VW * 4 < 16 ? VW * 4 : 16)));
-  if (blockIdx.x >= piece_blocks) {
-    constexpr int ZW = VW < 4 ? VW : 4;        // 16 bytes a store
-    typedef float zv_t __attribute__((ext_vector_type(ZW)));
-    const unsigned zpr = (unsigned)(H / ZW);
-    const uint64_t idx = (uint64_t)(blockIdx.x - piece_blocks) * 256 + threadIdx.x;
-    const uint64_t q = idx / zpr;
-    const int col = (int)(idx - q * zpr) * ZW;
-#pragma unroll
-    for (int k = 0; k < kZeroRows; ++k) {
-      const int64_t v = (int64_t)q * kZeroRows + k;
-      if (v >= V) break;
-      const int at = sh.place_of((int)v);
-      if (start[at] == start[at + 1]) __builtin_nontemporal_store(zv_t(0.f), reinterpret_cast<zv_t*>(G + v * ld_table + col));
-    }
-    return;
-  }
   const uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   const uint64_t p = idx / cpr;
   const int col = (int)(idx - p * cpr) * VW;
@@ -219,7 +228,8 @@ __global__ void __launch_bounds__(256) embed_rows_kernel(const int* __restrict__
       float* g = G + (int64_t)cur * ld_table + col;
       fv_t o = acc * scale;
       if (accumulate) o += *reinterpret_cast<const fv_t*>(g);
-      *reinterpret_cast<fv_t*>(g) = o;
+      if (STREAM) __builtin_nontemporal_store(o, reinterpret_cast<fv_t*>(g));
+      else *reinterpret_cast<fv_t*>(g) = o;
     }
     head = false;
   };
@@ -233,7 +243,10 @@ __global__ void __launch_bounds__(256) embed_rows_kernel(const int* __restrict__
       id[k] = sid[at];
     }
 #pragma unroll
-    for (int k = 0; k < U; ++k) r[k].load(dx + (int64_t)who[k] * ld_x + col);
+    for (int k = 0; k < U; ++k) {
+      if (STREAM) r[k].load_nt(dx + (int64_t)who[k] * ld_x + col);
+      else r[k].load(dx + (int64_t)who[k] * ld_x + col);
+    }
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       if (q + k >= to) break;
@@ -291,6 +304,77 @@ __global__ void __launch_bounds__(64 * kJoinWaves) embed_join_kernel(const int* 
   }
 }
 
+// A few tokens: one launch, no sort.  A workgroup per token and 64 VW columns lists the tokens with the same id; if its own is the first of them it
+// sums their rows, wavefront w the places w, w + 4, ... of the list, then the four in order.  The first zero_blocks workgroups zero the rows that no
+// token names.  Looking through the ids costs T * T / 64 loads for each column block, sorting them two launches more (few_tokens() has the line).
+constexpr int kFewTokens = 512, kZeroBlocks = 2048;
+template <typename T, int VW, typename TI>
+__global__ void __launch_bounds__(256) embed_few_kernel(const TI* __restrict__ ids, const T* __restrict__ dx, float* __restrict__ G, int T_, int H, int V, int64_t ld_table,
+                                                        int64_t ld_x, float scale, int accumulate, int zero_blocks) {
+  typedef float fv_t __attribute__((ext_vector_type(VW)));
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if ((int)blockIdx.x < zero_blocks) {
+    __shared__ unsigned named[(1 << 24) / kZeroBlocks / 32 + 1];
+    const int per = (V + zero_blocks - 1) / zero_blocks, v0 = blockIdx.x * per, n = V - v0 < per ? V - v0 : per;
+    for (int i = threadIdx.x; i <= per / 32; i += 256) named[i] = 0;
+    __syncthreads();
+    for (int t = threadIdx.x; t < T_; t += 256) {
+      const int r = row_id(ids, t, V) - v0;
+      if (r >= 0 && r < n) atomicOr(&named[r >> 5], 1u << (r & 31));
+    }
+    __syncthreads();
+    for (int r = wave; r < n; r += 4) {
+      if ((named[r >> 5] >> (r & 31)) & 1) continue;
+      float* g = G + (int64_t)(v0 + r) * ld_table;
+      for (int c = lane * VW; c < H; c += 64 * VW) __builtin_nontemporal_store(fv_t(0.f), reinterpret_cast<fv_t*>(g + c));
+    }
+    return;
+  }
+  __shared__ unsigned long long mask[kFewTokens / 64];
+  __shared__ int list[kFewTokens];
+  __shared__ fv_t red[4][64];
+  const unsigned b = blockIdx.x - zero_blocks, ncb = (unsigned)((H + 64 * VW - 1) / (64 * VW));
+  const int t = (int)(b / ncb), col = (int)(b % ncb) * 64 * VW + lane * VW;
+  const int v = row_id(ids, t, V), nb = (T_ + 63) / 64;
+  if (v < 0) return;
+  for (int i = wave; i < nb; i += 4) {
+    const int at = i * 64 + lane;
+    const unsigned long long same = __ballot(at < T_ && row_id(ids, at < T_ ? at : 0, V) == v);
+    if (lane == 0) mask[i] = same;
+  }
+  __syncthreads();
+  int n = 0;
+  for (int i = 0; i < nb; ++i) {
+    const unsigned long long same = mask[i];
+    if (i == (t >> 6) ? (same & ((1ull << (t & 63)) - 1)) != 0 : i < (t >> 6) && same) return;       // not the first
+    if ((i & 3) == wave && ((same >> lane) & 1)) list[n + __popcll(same & ((1ull << lane) - 1))] = i * 64 + lane;
+    n += __popcll(same);
+  }
+  __syncthreads();
+  fv_t acc = fv_t(0.f);
+  if (col < H) {
+    constexpr int U = 8;
+    for (int q = wave; q < n; q += 4 * U) {
+      Vec<T, VW> r[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k)
+        if (q + 4 * k < n) r[k].load(dx + (int64_t)list[q + 4 * k] * ld_x + col);
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        if (q + 4 * k >= n) break;
+#pragma unroll
+        for (int j = 0; j < VW; ++j) acc[j] += r[k].get(j);
+      }
+    }
+  }
+  red[wave][lane] = acc;
+  __syncthreads();
+  if (wave || col >= H) return;
+  acc = scale * (((acc + red[1][lane]) + red[2][lane]) + red[3][lane]);
+  fv_t* g = reinterpret_cast<fv_t*>(G + (int64_t)v * ld_table + col);
+  *g = accumulate ? *g + acc : acc;
+}
+
 // =============================================================================== launchers
 static inline int last_err() { return (int)hipGetLastError(); }
 
@@ -332,9 +416,9 @@ int launch_embed_fwd(const EmbedArgs& a, const void* ids, const void* table, voi
   });
 }
 
-// tokens of a piece: 32, or fewer where that leaves the chip fewer than 8 wavefronts a compute unit
+// tokens of a piece: 64, or fewer where that leaves the chip fewer than 8 wavefronts a compute unit
 static int piece_of(int64_t T_, int64_t cpr) {
-  int K = 32;
+  int K = 64;
   while (K > 8 && T_ * cpr < (int64_t)K * 131072) K /= 2;
   return K;
 }
@@ -356,43 +440,58 @@ static EmbedWork embed_work(const EmbedArgs& a, int K, void* base) {
   w.sid = (int*)take((size_t)a.T * 4);
   w.start = (int*)take((size_t)sort_shape(a.V).places() * 4);
   const size_t pieces = ((size_t)a.T + K - 1) / K;
-  w.part = (float*)take(pieces > 1 ? pieces * 2 * a.H * 4 : 0);
+  w.part = (float*)take(pieces * 2 * a.H * 4);
   w.bytes = off;
   return w;
 }
 
-size_t embed_bwd_workspace_bytes(const EmbedArgs& a) { return embed_work(a, piece_of(a.T, a.H / width_of(a.dtype, a.H, a.ld_table, a.ld_x)), nullptr).bytes; }
+constexpr uint64_t kStreamBytes = (uint64_t)64 << 20;       // dx: more than the L2 caches hold
+
+// columns of a thread of the backward
+static int bwd_width_of(const EmbedArgs& a) {
+  const int w = width_of(a.dtype, a.H, a.ld_table, a.ld_x);
+  return w < 4 ? w : 4;
+}
+
+// Rows of 4096 added to a shard, us without and with the sort: 128 tokens 4.7 and 20, 512 17 and 20, 1024 47 and 24; rows of 1024, 1024 tokens 16 and 19,
+// but all of one id 29 and 14, which is why there is a limit of its own on the tokens.
+static bool few_tokens(const EmbedArgs& a) { return a.T <= kFewTokens && (int64_t)a.T * a.T * ((a.H + 255) / 256) <= 1 << 22; }
+
+size_t embed_bwd_workspace_bytes(const EmbedArgs& a) { return few_tokens(a) ? 0 : embed_work(a, piece_of(a.T, a.H / bwd_width_of(a)), nullptr).bytes; }
 
 int launch_embed_bwd(const EmbedArgs& a, const void* ids, const void* dx, float* G, void* ws, hipStream_t st) {
   return by_types(a, [&](auto* t, auto* i, auto w) {
     using T = std::remove_pointer_t<decltype(t)>;
     using TI = std::remove_pointer_t<decltype(i)>;
-    constexpr int VW = decltype(w)::value;
+    constexpr int VW = decltype(w)::value < 4 ? decltype(w)::value : 4;
+    if (few_tokens(a)) {
+      const int zero = a.accumulate ? 0 : a.V < kZeroBlocks ? a.V : kZeroBlocks;
+      const uint64_t blocks = zero + (uint64_t)a.T * ((a.H + 64 * VW - 1) / (64 * VW));
+      if (blocks > 0x7fffffffu) return (int)hipErrorInvalidValue;
+      hipLaunchKernelGGL((embed_few_kernel<T, VW, TI>), dim3((unsigned)blocks), dim3(256), 0, st, (const TI*)ids, (const T*)dx, G, a.T, a.H, a.V, a.ld_table, a.ld_x, a.scale,
+                         a.accumulate, zero);
+      return last_err();
+    }
     const uint64_t cpr = a.H / VW;
     const int K = piece_of(a.T, (int64_t)cpr);
     const EmbedWork k = embed_work(a, K, ws);
     const SortShape sh = sort_shape(a.V);
     TAW_SET_LDS_LIMIT_ONCE((embed_sort_kernel<TI>), kSortWaves * kSortMaxOwn * sizeof(int));
-    hipLaunchKernelGGL((embed_sort_kernel<TI>), dim3(1u << sh.lb), dim3(1024), kSortWaves * sh.own * sizeof(int), st, (const TI*)ids, a.T, a.V, sh, k.perm, k.sid, k.start);
+    hipLaunchKernelGGL((embed_sort_kernel<TI>), dim3(1u << sh.lb), dim3(1024), kSortWaves * sh.own * sizeof(int), st, (const TI*)ids, a.T, a.V, sh, k.perm, k.sid, k.start,
+                       a.accumulate ? nullptr : G, a.H, a.ld_table);
     int e = last_err();
     if (e) return e;
     const uint64_t pieces = (a.T + K - 1) / K;
-    uint64_t pb, zb;
-    if (!grid_of(pieces * cpr, &pb) || !grid_of(a.accumulate ? 0 : (uint64_t)((a.V + kZeroRows - 1) / kZeroRows) * (a.H / (VW < 4 ? VW : 4)), &zb) || pb + zb > 0x7fffffffu) return (int)hipErrorInvalidValue;
-    if (pb + zb) {
-      hipLaunchKernelGGL((embed_rows_kernel<T, VW>), dim3((unsigned)(pb + zb)), dim3(256), 0, st, k.perm, k.sid, k.start, (const T*)dx, G, k.part, a.H, a.V, sh, a.ld_table, a.ld_x,
-                         a.scale, a.accumulate, K, (unsigned)pb);
-      e = last_err();
-      if (e) return e;
-    }
-    if (pieces > 1) {
-      constexpr int JW = VW < 4 ? VW : 4;
-      const unsigned cols = (unsigned)((a.H + 64 * JW - 1) / (64 * JW));
-      hipLaunchKernelGGL((embed_join_kernel<JW>), dim3((unsigned)((pieces + kJoinPieces - 1) / kJoinPieces), cols < 64 ? cols : 64), dim3(64 * kJoinWaves), 0, st, k.sid, k.start, k.part, G, a.H, sh, a.ld_table,
-                         a.scale, a.accumulate, K);
-      e = last_err();
-    }
-    return e;
+    uint64_t blocks;
+    if (!grid_of(pieces * cpr, &blocks)) return (int)hipErrorInvalidValue;
+    const auto rows = (uint64_t)a.T * a.H * sizeof(T) > kStreamBytes ? embed_rows_kernel<T, VW, true> : embed_rows_kernel<T, VW, false>;
+    hipLaunchKernelGGL(rows, dim3((unsigned)blocks), dim3(256), 0, st, k.perm, k.sid, k.start, (const T*)dx, G, k.part, a.H, sh, a.ld_table, a.ld_x, a.scale, a.accumulate, K);
+    e = last_err();
+    if (e) return e;
+    const unsigned cols = (unsigned)((a.H + 64 * VW - 1) / (64 * VW));
+    hipLaunchKernelGGL((embed_join_kernel<VW>), dim3((unsigned)((pieces + kJoinPieces - 1) / kJoinPieces), cols < 64 ? cols : 64), dim3(64 * kJoinWaves), 0, st, k.sid, k.start,
+                       k.part, G, a.H, sh, a.ld_table, a.scale, a.accumulate, K);
+    return last_err();
   });
 }
 

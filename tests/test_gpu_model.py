@@ -40,7 +40,7 @@ def zipf_ids(rng, T, V):
 
 EMBED = [  # T, H, V
     (1, 1, 1), (1, 64, 509), (5, 7, 3), (63, 64, 5), (64, 8, 1000), (65, 100, 7), (128, 64, 509), (257, 520, 33), (333, 256, 32003),
-    (1000, 1, 2), (1025, 72, 64), (1500, 1032, 300), (2049, 513, 20000), (4503, 1024, 32001)]
+    (1000, 1, 2), (1024, 264, 70), (1025, 72, 64), (1100, 6, 300001), (1500, 1032, 300), (2049, 513, 20000), (4503, 1024, 32001), (9001, 20, 5), (20000, 8, 1)]
 
 
 @pytest.mark.parametrize("T,H,V", EMBED)
@@ -102,6 +102,23 @@ def test_embed_strides_and_what_lies_between(taw, T, V, H):
         ref = M.embed_bwd(ids, f64(x[:, :H]), V)
         size = M.embed_bwd(ids, np.abs(f64(x[:, :H])), V)
         assert np.all(np.abs(f64(G[:, :H]) - ref) <= T * u * size) and bool((G[:, H:] == 3.0).all())
+
+
+def test_embed_bwd_past_the_caches(taw):
+    """Gradients that no cache holds, which the kernels stream."""
+    T, H, V = 9000, 4096, 600
+    rng = np.random.default_rng(6)
+    ids, dx = zipf_ids(rng, T, V), torch.randn((T, H), device="cuda", dtype=torch.bfloat16)
+    for accumulate in (False, True):
+        G = torch.randn((V, H), device="cuda")
+        d = taw.make_embed_desc(taw.TAW_BF16, T, H, V, flags=taw.TAW_ACCUMULATE if accumulate else 0)
+        ref, size = (G.double(), G.double().abs()) if accumulate else (torch.zeros(V, H, dtype=torch.float64, device="cuda") for _ in range(2))
+        for v in range(V):
+            rows = dx[torch.from_numpy(np.flatnonzero(ids == v)).cuda()].double()
+            ref[v] += rows.sum(0)
+            size[v] += rows.abs().sum(0)
+        taw.taw_embed_bwd(d, on_gpu(ids, torch.int32), dx, G, scratch(taw.taw_embed_bwd_workspace_bytes(d)))
+        assert bool(((G.double() - ref).abs() <= (int(np.bincount(ids).max()) + 2) * u * size).all())
 
 
 def test_embed_bwd_repeats_its_bits_and_no_tokens_zero_the_shard(taw):

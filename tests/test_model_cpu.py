@@ -156,10 +156,14 @@ def test_embedding_refusals(lib):
     refuse(taw.TAW_ERR_SHAPE, taw.taw_embed_fwd, d, far + 16, OK, far)                              # x over the ids
     refuse(taw.TAW_ERR_SHAPE, taw.taw_embed_bwd, d, far, OK, OK, far + (1 << 20), ws)               # G over dx
     refuse(taw.TAW_ERR_SHAPE, taw.taw_embed_bwd, d, OK, far, OK + 16, far + (1 << 20), ws)          # G over the ids
-    if ws:
-        refuse(taw.TAW_ERR_WORKSPACE, taw.taw_embed_bwd, d, OK, far, far + (1 << 20), far + (1 << 22), ws - 1)
-        refuse(taw.TAW_ERR_NULL, taw.taw_embed_bwd, d, OK, far, far + (1 << 20), None, ws)
-        refuse(taw.TAW_ERR_SHAPE, taw.taw_embed_bwd, d, OK, far, far + (1 << 20), far, ws)
+    assert ws == 0                                                                                  # a few tokens need none
+    more = taw.make_embed_desc(taw.TAW_BF16, 5000, 64, 100)
+    ws = taw.taw_embed_bwd_workspace_bytes(more)
+    assert ws > 0
+    refuse(taw.TAW_ERR_WORKSPACE, taw.taw_embed_bwd, more, OK, far, far + (1 << 20), far + (1 << 22), ws - 1)
+    refuse(taw.TAW_ERR_NULL, taw.taw_embed_bwd, more, OK, far, far + (1 << 20), None, ws)
+    refuse(taw.TAW_ERR_ALIGN, taw.taw_embed_bwd, more, OK, far, far + (1 << 20), far + (1 << 22) + 8, ws)
+    refuse(taw.TAW_ERR_SHAPE, taw.taw_embed_bwd, more, OK, far, far + (1 << 20), far, ws)
     none = taw.make_embed_desc(taw.TAW_BF16, 0, 64, 100, flags=taw.TAW_ACCUMULATE)
     taw.taw_embed_fwd(none, None, None, None)                                                       # no tokens: nothing to do
     taw.taw_embed_bwd(none, None, None, None, None)
