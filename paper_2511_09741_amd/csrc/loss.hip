@@ -12,12 +12,15 @@ namespace taw {
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kInf = __builtin_huge_valf();
 
-// the label of row t, or -1 where the row is not counted
-template <typename TI>
-__device__ __forceinline__ int label_of(const TI* __restrict__ labels, int64_t t, int V) {
-  const TI y = labels[t];
-  return y >= 0 && y < (TI)V ? (int)y : -1;
-}
+// the label of a row, or -1 where the row is not counted
+struct Labels {
+  const void* p;
+  int wide, V;                // int64
+  __device__ __forceinline__ int operator[](int64_t t) const {
+    const int64_t y = wide ? static_cast<const int64_t*>(p)[t] : static_cast<const int32_t*>(p)[t];
+    return y >= 0 && y < V ? (int)y : -1;
+  }
+};
 
 // sum and maximum over a workgroup of NW wavefronts, for every thread, in wavefront order
 template <int NW>
@@ -49,11 +52,10 @@ struct RowTerms {                 // of the loss
 };
 
 // =============================================================================== counted rows
-template <typename TI>
-__global__ void __launch_bounds__(1024) loss_count_kernel(const TI* __restrict__ labels, int T_, int V, int* __restrict__ count) {
+__global__ void __launch_bounds__(1024) loss_count_kernel(const Labels labels, int T_, int* __restrict__ count) {
   __shared__ int red[16];
   int n = 0;
-  for (int t = threadIdx.x; t < T_; t += 1024) n += label_of(labels, t, V) >= 0;
+  for (int t = threadIdx.x; t < T_; t += 1024) n += labels[t] >= 0;
   for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
   __syncthreads();
@@ -65,55 +67,50 @@ __global__ void __launch_bounds__(1024) loss_count_kernel(const TI* __restrict__
 }
 
 // =============================================================================== a row as vectors
-// A row is taken as 16-byte vectors aligned in memory, whatever its first element is aligned to: the first vector starts `lead` elements before the
-// row, and what of the first and the last one lies outside the row is neither read nor written.
-template <typename TL, typename TG>
+// A row is taken as `count` vectors of 16 bytes that are aligned in memory, whatever its first element is aligned to, and the up to VW - 1 elements
+// before and behind them, its edge, of which each of the first threads has one.  SAME: the gradient's rows start as far from a vector as the logits',
+// so that its vectors are aligned too; without it they are stored element by element.
+template <typename TL, typename TG, bool SAME>
 struct RowVecs {
   static constexpr int VW = 16 / sizeof(TL);
+  typedef Vec<TL, VW> vec_t;
+  static constexpr bool kHoldsExp = sizeof(TL) == 4;
   const TL* in;               // the first vector
   TG* out;                    // the gradient at the same place
-  int lead, end, count;       // elements [lead, end) of the vectors are the row
-  bool wide;                  // the gradient's vectors are aligned too
-  typedef Vec<TL, VW> vec_t;
+  int head, count, tail;      // elements before the vectors, vectors, elements behind them
 
   __device__ __forceinline__ RowVecs(const TL* logits, TG* dlogits, int64_t t, int V, int64_t ld, int64_t ld_grad) {
-    const int64_t at = t * ld;
-    lead = (int)(at & (VW - 1));
-    end = lead + V;
-    count = (end + VW - 1) / VW;
-    in = logits + (at - lead);
-    const int64_t to = t * ld_grad - lead;
-    out = dlogits + to;
-    wide = (to & (VW - 1)) == 0;
+    const int64_t at = t * ld, to = t * ld_grad;
+    head = (int)(-at & (VW - 1));
+    head = head < V ? head : V;
+    count = (V - head) / VW;
+    tail = V - head - count * VW;
+    in = logits + (at + head);
+    out = dlogits + (to + head);
   }
-  __device__ __forceinline__ bool inside(int c) const { return c * VW >= lead && (c + 1) * VW <= end; }
-  // outside the row: -inf, a class of probability 0
-  __device__ __forceinline__ void load(int c, vec_t& x) const {
-    if (inside(c)) {
-      x.load_nt(in + (int64_t)c * VW);
-    } else {
-#pragma unroll
-      for (int j = 0; j < VW; ++j) {
-        const int e = c * VW + j;
-        x.set(j, -kInf);
-        if (e >= lead && e < end) x.raw[j] = in[e];
-      }
-    }
+  // KEEP: leave it in the caches, it will be read again
+  template <bool KEEP = false>
+  __device__ __forceinline__ void load(unsigned c, vec_t& x) const {
+    if (KEEP) x.load(in + (size_t)c * VW);
+    else x.load_nt(in + (size_t)c * VW);
   }
-  __device__ __forceinline__ void store(int c, const float* g) const {
-    if (wide && inside(c)) {
+  __device__ __forceinline__ void store(unsigned c, const float* g) const {
+    if (SAME) {
       typedef TG out_t __attribute__((ext_vector_type(VW)));
       out_t o;
 #pragma unroll
       for (int j = 0; j < VW; ++j) o[j] = (TG)g[j];
-      __builtin_nontemporal_store(o, reinterpret_cast<out_t*>(out + (int64_t)c * VW));
+      __builtin_nontemporal_store(o, reinterpret_cast<out_t*>(out + (size_t)c * VW));
     } else {
 #pragma unroll
-      for (int j = 0; j < VW; ++j) {
-        const int e = c * VW + j;
-        if (e >= lead && e < end) out[e] = (TG)g[j];
-      }
+      for (int j = 0; j < VW; ++j) out[(size_t)c * VW + j] = (TG)g[j];
     }
+  }
+  // this thread's element of the edge, relative to the first vector; there is none where edge() is false
+  __device__ __forceinline__ bool edge(int* e) const {
+    const int i = threadIdx.x;
+    *e = i < head ? i - head : i - head + count * VW;
+    return i < head + tail;
   }
 };
 
@@ -128,159 +125,240 @@ struct Shift {
   __device__ __forceinline__ float lse(float m, float sum) const { return huge ? m + logf(sum) : (ms + log2f(sum)) * kLn2; }
 };
 
-// the gradient of VW logits: scale * exp(l) - share, and less by `own` at the label
+// A vector that a row's workgroup holds.  fp32: the exponentials take the place of the logits, and are not formed a second time for the gradient (which
+// took a third of the kernel's instructions).  bf16: they would take twice the registers, so the logits stay.
 template <typename R>
-__device__ __forceinline__ void gradient(const R& row, int c, const typename R::vec_t& x, const Shift& sh, float scale, float share, float own, int y) {
+__device__ __forceinline__ void sum_exp(typename R::vec_t& x, const Shift& sh, float& sum) {
+#pragma unroll
+  for (int j = 0; j < R::VW; ++j) {
+    const float e = sh.exp(x.get(j));
+    sum += e;
+    if (R::kHoldsExp) x.set(j, e);
+  }
+}
+
+// the gradient of VW logits: scale * exp(l) - share, and less by `own` at the label.  HELD: sum_exp() has seen the vector
+template <bool HELD, typename R>
+__device__ __forceinline__ void gradient(const R& row, unsigned c, const typename R::vec_t& x, const Shift& sh, float scale, float share, float own, int y) {
   float g[R::VW];
 #pragma unroll
-  for (int j = 0; j < R::VW; ++j) g[j] = __builtin_fmaf(scale, sh.exp(x.get(j)), -share);
-  const int at = y + row.lead - c * R::VW;
-  if (at >= 0 && at < R::VW) {
+  for (int j = 0; j < R::VW; ++j) g[j] = __builtin_fmaf(scale, HELD && R::kHoldsExp ? x.get(j) : sh.exp(x.get(j)), -share);
+  const unsigned at = (unsigned)(y - row.head) - c * R::VW;
+  if (at < (unsigned)R::VW) {
 #pragma unroll
     for (int j = 0; j < R::VW; ++j)
-      if (j == at) g[j] -= own;
+      if (j == (int)at) g[j] -= own;
   }
   row.store(c, g);
 }
 
+// what a row comes to, from its maximum m, its sum of exponentials and (label smoothing) its sum of logits; thread 0 stores it
+struct RowResult {
+  float scale, share, own;                         // gradient: scale * exp(l) - share, - own at the label
+  __device__ __forceinline__ RowResult(const Shift& sh, float m, float sum, float total, float ly, int V, const RowTerms& c, float counted, int64_t t,
+                                       float* __restrict__ rows, float* __restrict__ lse_out) {
+    const bool none = sum == 0.f;                  // nothing but -inf
+    const float lse = none ? -kInf : sh.lse(m, sum);
+    if (threadIdx.x == 0) {
+      float r = none ? kInf : lse - (1.f - c.eps) * ly;
+      if (c.eps != 0.f) r -= c.eps / (float)V * total;
+      if (c.z != 0.f) r += c.z * lse * lse;
+      rows[t] = r;
+      if (lse_out) lse_out[t] = lse;
+    }
+    const float up = none ? 0.f : c.mean ? c.grad_scale / counted : c.grad_scale;
+    scale = none ? 0.f : up * (c.z != 0.f ? 1.f + 2.f * c.z * lse : 1.f) / sum;
+    share = up * c.eps / (float)V;
+    own = up * (1.f - c.eps);
+  }
+};
+
+// The maximum of a held row of bf16, two values an instruction: as signed integers the bits of floats that are not negative are in the floats' order,
+// and above those of the negative ones.  Where the row's maximum is negative (none() after the workgroup's maximum) it is formed in floats after all.
+typedef short s16x2_t __attribute__((ext_vector_type(2)));
+template <typename R>
+struct PairMax {
+  s16x2_t m = {-32768, -32768};
+  __device__ __forceinline__ void add(const typename R::vec_t& x) {
+    const u32x4_t w = __builtin_bit_cast(u32x4_t, x.raw);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const unsigned two = w[j];
+      m = __builtin_elementwise_max(m, __builtin_bit_cast(s16x2_t, two));
+    }
+  }
+  __device__ __forceinline__ float top() const {
+    const int i = m[0] > m[1] ? m[0] : m[1];
+    return i >= 0 ? __uint_as_float((unsigned)i << 16) : -kInf;
+  }
+  static __device__ __forceinline__ bool none(float top) { return !(top >= 0.f); }
+};
+
+// the edge of a row: a logit a thread, -inf (a class of probability 0) where it has none
+template <typename R>
+struct Edge {
+  int e;
+  bool have;
+  float l;
+  __device__ __forceinline__ Edge(const R& row, float eps, float& top, float& total) {
+    have = row.edge(&e);
+    l = have ? (float)row.in[e] : -kInf;
+    top = fmaxf(top, l);
+    if (have && eps != 0.f) total += l;
+  }
+  template <typename G>
+  __device__ __forceinline__ void store(const R& row, const Shift& sh, const G& g, int y) const {
+    if (have) row.out[e] = __builtin_fmaf(g.scale, sh.exp(l), -g.share) - (e + row.head == y ? g.own : 0.f);
+  }
+};
+
+// a row that is not counted
+template <int NT, bool GRAD, bool SAME, typename TL, typename TG>
+__device__ __forceinline__ void empty_row(const TL* logits, TG* dlogits, int64_t t, int V, int V_pad, int64_t ld, int64_t ld_grad, float* __restrict__ rows,
+                                          float* __restrict__ lse_out) {
+  typedef RowVecs<TL, TG, SAME> R;
+  if (threadIdx.x == 0) {
+    rows[t] = 0.f;
+    if (lse_out) lse_out[t] = 0.f;
+  }
+  if (!GRAD) return;
+  const R row(logits, dlogits, t, V, ld, ld_grad);
+  const float zero[R::VW] = {};
+  for (int i = threadIdx.x; i < row.count; i += NT) row.store(i, zero);
+  int e;
+  if (row.edge(&e)) row.out[e] = (TG)0.f;
+  for (int v = V + threadIdx.x; v < V_pad; v += NT) dlogits[t * ld_grad + v] = (TG)0.f;
+}
+
 // =============================================================================== rows
 // A workgroup of NT threads per row, which stays packed in registers (MAXC vectors a thread) between its maximum, its sum of exponentials and its
-// gradient: the logits are read once.  What does not fit (MORE) is summed on the way with a running maximum, and read a second time for the gradient.
-template <typename TL, typename TG, typename TI, int NT, int MAXC, bool MORE, bool GRAD>
-__global__ void __launch_bounds__(NT) loss_row_kernel(const TL* logits, const TI* __restrict__ labels, int T_, int V, int V_pad, int64_t ld, int64_t ld_grad, RowTerms c,
+// gradient: the logits are read once.  MORE: of a row that is longer, the rest is summed on the way with a running maximum, and read a second time for the
+// gradient, backwards (what was read last is the likeliest to be in a cache).
+template <typename TL, typename TG, int NT, int MAXC, bool MORE, bool GRAD, bool SAME>
+__global__ void __launch_bounds__(NT) loss_row_kernel(const TL* logits, const Labels labels, int T_, int V, int V_pad, int64_t ld, int64_t ld_grad, RowTerms c,
                                                       const int* __restrict__ count, float* __restrict__ rows, float* __restrict__ lse_out, TG* dlogits) {
-  typedef RowVecs<TL, TG> R;
+  typedef RowVecs<TL, TG, SAME> R;
   constexpr int NW = NT / 64;
   __shared__ float red[NW];
   const int64_t t = blockIdx.x;
-  const int y = label_of(labels, t, V), tid = threadIdx.x;
+  const int y = labels[t], tid = threadIdx.x;
   if (y < 0) {
-    if (tid == 0) {
-      rows[t] = 0.f;
-      if (lse_out) lse_out[t] = 0.f;
-    }
-    if (GRAD) {
-      const R row(logits, dlogits, t, V, ld, ld_grad);
-      const float zero[R::VW] = {};
-      for (int i = tid; i < row.count; i += NT) row.store(i, zero);
-      for (int v = V + tid; v < V_pad; v += NT) dlogits[t * ld_grad + v] = (TG)0.f;
-    }
+    empty_row<NT, GRAD, SAME>(logits, dlogits, t, V, V_pad, ld, ld_grad, rows, lse_out);
     return;
   }
   const R row(logits, dlogits, t, V, ld, ld_grad);
   const float ly = (float)logits[t * ld + y];      // before anything is written: dlogits may be the logits
+  typename R::vec_t x[MAXC];
+  if (row.count)
+#pragma unroll
+    for (int k = 0; k < MAXC; ++k) row.load(tid + k * NT < row.count ? tid + k * NT : row.count - 1, x[k]);      // always a load: none waits for a branch
   float counted = 1.f;
   if (GRAD && c.mean) {
     if (count) {
       counted = (float)*count;
     } else {
       int n = 0;
-      for (int i = tid; i < T_; i += NT) n += label_of(labels, i, V) >= 0;
+      for (int i = tid; i < T_; i += NT) n += labels[i] >= 0;
       counted = block_sum<NW>((float)n, red);      // exact: T is small here
     }
   }
   float top = -kInf, total = 0.f, sum = 0.f;
+  const int n = row.count > tid ? (row.count - tid + NT - 1) / NT : 0;                 // vectors of this thread
   if (MORE) {
     constexpr int U = 4;
-    for (int i = tid + MAXC * NT; i < row.count; i += U * NT) {
-      typename R::vec_t x[U];
+    for (int k0 = MAXC; k0 < n; k0 += U) {
+      typename R::vec_t z[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) row.template load<true>(tid + (k0 + k < n ? k0 + k : k0) * NT, z[k]);
+      const float was = top;
 #pragma unroll
       for (int k = 0; k < U; ++k)
-        if (i + k * NT < row.count) row.load(i + k * NT, x[k]);
-      float m = top;
+        if (k0 + k < n)
+#pragma unroll
+          for (int j = 0; j < R::VW; ++j) top = fmaxf(top, z[k].get(j));
+      const float ref = top == -kInf ? 0.f : top;
+      sum *= __builtin_amdgcn_exp2f((was - ref) * kLog2e);
 #pragma unroll
       for (int k = 0; k < U; ++k)
-        if (i + k * NT < row.count)
-#pragma unroll
-          for (int j = 0; j < R::VW; ++j) m = fmaxf(m, x[k].get(j));
-      const float ref = m == -kInf ? 0.f : m;
-      sum *= __builtin_amdgcn_exp2f((top - ref) * kLog2e);
-#pragma unroll
-      for (int k = 0; k < U; ++k)
-        if (i + k * NT < row.count)
+        if (k0 + k < n)
 #pragma unroll
           for (int j = 0; j < R::VW; ++j) {
-            const float l = x[k].get(j);
+            const float l = z[k].get(j);
             sum += __builtin_amdgcn_exp2f((l - ref) * kLog2e);
-            const int e = (i + k * NT) * R::VW + j;
-            if (c.eps != 0.f && e >= row.lead && e < row.end) total += l;
+            if (c.eps != 0.f) total += l;
           }
-      top = m;
     }
   }
-  typename R::vec_t x[MAXC];
+  const float before = top;                        // what sum is relative to
+  const Edge<R> edge(row, c.eps, top, total);
+  const auto exact_top = [&]() {
 #pragma unroll
-  for (int k = 0; k < MAXC; ++k)
-    if (tid + k * NT < row.count) row.load(tid + k * NT, x[k]);
-  const float mine = top;
+    for (int k = 0; k < MAXC; ++k)
+      if (k < n)
 #pragma unroll
-  for (int k = 0; k < MAXC; ++k)
-    if (tid + k * NT < row.count) {
+        for (int j = 0; j < R::VW; ++j) top = fmaxf(top, x[k].get(j));
+    return block_max<NW>(top, red);
+  };
+  if constexpr (sizeof(TL) == 2) {
+    PairMax<R> pairs;
 #pragma unroll
-      for (int j = 0; j < R::VW; ++j) top = fmaxf(top, x[k].get(j));
-      if (c.eps != 0.f)
+    for (int k = 0; k < MAXC; ++k)
+      if (k < n) pairs.add(x[k]);
+    const float all = block_max<NW>(fmaxf(top, pairs.top()), red);
+    top = pairs.none(all) ? exact_top() : all;
+  } else {
+    top = exact_top();
+  }
+  if (c.eps != 0.f) {
 #pragma unroll
-        for (int j = 0; j < R::VW; ++j) {
-          const int e = (tid + k * NT) * R::VW + j;
-          if (e >= row.lead && e < row.end) total += x[k].get(j);
-        }
-    }
-  top = block_max<NW>(top, red);
+    for (int k = 0; k < MAXC; ++k)
+      if (k < n)
+#pragma unroll
+        for (int j = 0; j < R::VW; ++j) total += x[k].get(j);
+    total = block_sum<NW>(total, red);
+  }
   const float m = top == -kInf ? 0.f : top;
   const Shift sh(m);
-  if (MORE) sum *= sh.exp(mine);
+  if (MORE && n > MAXC) sum *= sh.exp(before);
+  sum += sh.exp(edge.l);
 #pragma unroll
   for (int k = 0; k < MAXC; ++k) {
     x[k].pin();
-    if (tid + k * NT < row.count)
-#pragma unroll
-      for (int j = 0; j < R::VW; ++j) sum += sh.exp(x[k].get(j));
+    if (k < n) sum_exp<R>(x[k], sh, sum);
   }
   sum = block_sum<NW>(sum, red);
-  if (c.eps != 0.f) total = block_sum<NW>(total, red);
-  const float lse = sum == 0.f ? -kInf : sh.lse(m, sum);
-  if (tid == 0) {
-    float r = sum == 0.f ? kInf : lse - (1.f - c.eps) * ly;
-    if (c.eps != 0.f) r -= c.eps / (float)V * total;
-    if (c.z != 0.f) r += c.z * lse * lse;
-    rows[t] = r;
-    if (lse_out) lse_out[t] = lse;
-  }
+  const RowResult g(sh, m, sum, total, ly, V, c, counted, t, rows, lse_out);
   if (!GRAD) return;
-  const bool none = sum == 0.f;                    // nothing but -inf
-  const float up = none ? 0.f : c.mean ? c.grad_scale / counted : c.grad_scale;
-  const float scale = none ? 0.f : up * (c.z != 0.f ? 1.f + 2.f * c.z * lse : 1.f) / sum, share = up * c.eps / (float)V, own = up * (1.f - c.eps);
 #pragma unroll
   for (int k = 0; k < MAXC; ++k) {
     x[k].pin();
-    if (tid + k * NT < row.count) gradient(row, tid + k * NT, x[k], sh, scale, share, own, y);
+    if (k < n) gradient<true>(row, tid + k * NT, x[k], sh, g.scale, g.share, g.own, y);
   }
   if (MORE) {
-    constexpr int U = 4;                           // backwards: what was read last is the likeliest to be in a cache
-    const int n = (row.count - tid + NT - 1) / NT;
+    constexpr int U = 4;
     for (int k0 = n - 1; k0 >= MAXC; k0 -= U) {
       typename R::vec_t z[U];
 #pragma unroll
-      for (int k = 0; k < U; ++k)
-        if (k0 - k >= MAXC) row.load(tid + (k0 - k) * NT, z[k]);
+      for (int k = 0; k < U; ++k) row.load(tid + (k0 - k >= MAXC ? k0 - k : k0) * NT, z[k]);
 #pragma unroll
       for (int k = 0; k < U; ++k)
-        if (k0 - k >= MAXC) gradient(row, tid + (k0 - k) * NT, z[k], sh, scale, share, own, y);
+        if (k0 - k >= MAXC) gradient<false>(row, tid + (k0 - k) * NT, z[k], sh, g.scale, g.share, g.own, y);
     }
   }
+  edge.store(row, sh, g, y);
   for (int v = V + tid; v < V_pad; v += NT) dlogits[t * ld_grad + v] = (TG)0.f;
 }
 
 // The gradient from a saved lse: nothing is summed, so a row is cut into parts of kPart vectors.
 constexpr int kPart = 1024;
-template <typename TL, typename TG, typename TI>
-__global__ void __launch_bounds__(256) loss_bwd_kernel(const TL* logits, const TI* __restrict__ labels, int V, int V_pad, int64_t ld, int64_t ld_grad, RowTerms c,
+template <typename TL, typename TG, bool SAME>
+__global__ void __launch_bounds__(256) loss_bwd_kernel(const TL* logits, const Labels labels, int V, int V_pad, int64_t ld, int64_t ld_grad, RowTerms c,
                                                        const float* __restrict__ lse_in, const float* __restrict__ dloss, TG* dlogits, unsigned parts) {
-  typedef RowVecs<TL, TG> R;
+  typedef RowVecs<TL, TG, SAME> R;
   constexpr int U = kPart / 256;
   const int64_t t = blockIdx.x / parts;
   const unsigned part = blockIdx.x - (unsigned)t * parts;
-  const int y = label_of(labels, t, V);
+  const int y = labels[t];
   const R row(logits, dlogits, t, V, ld, ld_grad);
   const float lse = lse_in[t];
   const bool none = y < 0 || lse == -kInf;
@@ -293,9 +371,10 @@ __global__ void __launch_bounds__(256) loss_bwd_kernel(const TL* logits, const T
   }
   const Shift sh(lse);
   const float up = none ? 0.f : dloss[t];
-  // what the rounding of lse s leaves out
-  const float rest = sh.huge ? 1.f : __builtin_amdgcn_exp2f(-__builtin_fmaf(lse, sh.s, -sh.ms));
-  const float scale = up * (c.z != 0.f ? 1.f + 2.f * c.z * lse : 1.f) * rest, share = up * c.eps / (float)V, own = up * (1.f - c.eps);
+  const float rest = sh.huge ? 1.f : __builtin_amdgcn_exp2f(-__builtin_fmaf(lse, sh.s, -sh.ms));     // what the rounding of lse s leaves out
+  struct {
+    float scale, share, own;
+  } const g{up * (c.z != 0.f ? 1.f + 2.f * c.z * lse : 1.f) * rest, up * c.eps / (float)V, up * (1.f - c.eps)};
 #pragma unroll
   for (int k = 0; k < U; ++k) {
     const int i = first + k * 256;
@@ -304,23 +383,24 @@ __global__ void __launch_bounds__(256) loss_bwd_kernel(const TL* logits, const T
       const float zero[R::VW] = {};
       row.store(i, zero);
     } else {
-      gradient(row, i, x[k], sh, scale, share, own, y);
+      gradient<false>(row, i, x[k], sh, g.scale, g.share, g.own, y);
     }
   }
-  if (part == parts - 1)
-    for (int v = V + threadIdx.x; v < V_pad; v += 256) dlogits[t * ld_grad + v] = (TG)0.f;
+  if (part) return;
+  int e;
+  if (row.edge(&e)) row.out[e] = none ? 0.f : __builtin_fmaf(g.scale, sh.exp((float)row.in[e]), -g.share) - (e + row.head == y ? g.own : 0.f);
+  for (int v = V + threadIdx.x; v < V_pad; v += 256) dlogits[t * ld_grad + v] = (TG)0.f;
 }
 
 // =============================================================================== sum of the rows' losses
-template <typename TI>
-__global__ void __launch_bounds__(1024) loss_sum_kernel(const float* __restrict__ rows, const TI* __restrict__ labels, int T_, int V, int mean, float* __restrict__ loss) {
+__global__ void __launch_bounds__(1024) loss_sum_kernel(const float* __restrict__ rows, const Labels labels, int T_, int mean, float* __restrict__ loss) {
   __shared__ double red[16];
   __shared__ int redn[16];
   double s = 0.0;
   int n = 0;
   for (int t = threadIdx.x; t < T_; t += 1024) {
     s += (double)rows[t];
-    n += label_of(labels, t, V) >= 0;
+    n += labels[t] >= 0;
   }
   for (int o = 32; o > 0; o >>= 1) {
     s += __shfl_xor(s, o, 64);
@@ -350,61 +430,63 @@ size_t loss_workspace_bytes(int T_) { return 256 + ((size_t)T_ * 4 + 255) / 256 
 
 template <typename F>
 static int by_types(const LossArgs& a, F f) {
-  const auto with_labels = [&](auto* l, auto* g) { return a.label_type == IDX_I64 ? f(l, g, (int64_t*)nullptr) : f(l, g, (int32_t*)nullptr); };
-  if (a.dtype == DT_BF16) return with_labels((bf16_t*)nullptr, (bf16_t*)nullptr);
-  if (a.grad_dtype == DT_BF16) return with_labels((float*)nullptr, (bf16_t*)nullptr);
-  return with_labels((float*)nullptr, (float*)nullptr);
+  const auto with = [&](auto* l, auto* g) {
+    constexpr int64_t VW = 16 / sizeof(*l);
+    return (a.ld - a.ld_grad) % VW == 0 ? f(l, g, std::true_type{}) : f(l, g, std::false_type{});
+  };
+  if (a.dtype == DT_BF16) return with((bf16_t*)nullptr, (bf16_t*)nullptr);
+  if (a.grad_dtype == DT_BF16) return with((float*)nullptr, (bf16_t*)nullptr);
+  return with((float*)nullptr, (float*)nullptr);
 }
 
 // rows up to which a workgroup counts the labels itself: a launch costs more than reading this many
 constexpr int kCountedInline = 2048;
 
 int launch_loss(const LossArgs& a, const void* logits, const void* labels, float* loss, float* rows, float* lse, void* dlogits, void* ws, hipStream_t st) {
-  int* count = dlogits && a.mean && a.T > kCountedInline ? (int*)ws : nullptr;
+  int* count = (int*)ws;
   if (!rows) rows = (float*)((char*)ws + 256);
   const RowTerms c{a.eps, a.z, a.grad_scale, a.mean};
-  return by_types(a, [&](auto* pl, auto* pg, auto* pi) {
+  const Labels y{labels, a.label_type == IDX_I64, a.V};
+  return by_types(a, [&](auto* pl, auto* pg, auto same) {
     using TL = std::remove_pointer_t<decltype(pl)>;
     using TG = std::remove_pointer_t<decltype(pg)>;
-    using TI = std::remove_pointer_t<decltype(pi)>;
+    constexpr bool SAME = decltype(same)::value;
+    const TL* l = (const TL*)logits;
+    TG* d = (TG*)dlogits;
     if (a.T) {
-      if (count) hipLaunchKernelGGL((loss_count_kernel<TI>), dim3(1), dim3(1024), 0, st, (const TI*)labels, a.T, a.V, count);
       constexpr int VW = 16 / sizeof(TL);
-      const int vecs = (a.V + 2 * (VW - 1)) / VW;      // at most, wherever a row starts
-#define TAW_LOSS(NT, MAXC, MORE)                                                                                                                                    \
-  do {                                                                                                                                                              \
-    if (dlogits)                                                                                                                                                    \
-      hipLaunchKernelGGL((loss_row_kernel<TL, TG, TI, NT, MAXC, MORE, true>), dim3((unsigned)a.T), dim3(NT), 0, st, (const TL*)logits, (const TI*)labels, a.T, a.V,  \
-                         a.V_pad, a.ld, a.ld_grad, c, count, rows, lse, (TG*)dlogits);                                                                              \
-    else                                                                                                                                                            \
-      hipLaunchKernelGGL((loss_row_kernel<TL, TG, TI, NT, MAXC, MORE, false>), dim3((unsigned)a.T), dim3(NT), 0, st, (const TL*)logits, (const TI*)labels, a.T, a.V, \
-                         a.V_pad, a.ld, a.ld_grad, c, count, rows, lse, (TG*)nullptr);                                                                              \
+      const int vecs = a.V / VW;
+      if (d && a.mean && a.T > kCountedInline) hipLaunchKernelGGL(loss_count_kernel, dim3(1), dim3(1024), 0, st, y, a.T, count);
+      else count = nullptr;
+#define TAW_LOSS(NT, MAXC, MORE)                                                                                                                    \
+  do {                                                                                                                                              \
+    const auto kernel = d ? loss_row_kernel<TL, TG, NT, MAXC, MORE, true, SAME> : loss_row_kernel<TL, TG, NT, MAXC, MORE, false, true>;             \
+    hipLaunchKernelGGL(kernel, dim3((unsigned)a.T), dim3(NT), 0, st, l, y, a.T, a.V, a.V_pad, a.ld, a.ld_grad, c, count, rows, lse, d);             \
   } while (0)
       if (vecs <= 64 * 8) TAW_LOSS(64, 8, false);
       else if (vecs <= 256 * 8) TAW_LOSS(256, 8, false);
       else if (vecs <= 512 * 8) TAW_LOSS(512, 8, false);
-      else if (vecs <= 1024 * 8) TAW_LOSS(1024, 8, false);
-      else if (vecs <= 1024 * 16) TAW_LOSS(1024, 16, false);
-      else TAW_LOSS(1024, 16, true);
+      else if (vecs <= 512 * 16) TAW_LOSS(512, 16, false);
+      else TAW_LOSS(512, 16, true);
 #undef TAW_LOSS
       const int e = last_err();
       if (e) return e;
     }
-    hipLaunchKernelGGL((loss_sum_kernel<TI>), dim3(1), dim3(1024), 0, st, rows, (const TI*)labels, a.T, a.V, a.mean, loss);
+    hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, st, rows, y, a.T, a.mean, loss);
     return last_err();
   });
 }
 
 int launch_loss_bwd(const LossArgs& a, const void* logits, const void* labels, const float* lse, const float* dloss, void* dlogits, hipStream_t st) {
   const RowTerms c{a.eps, a.z, 0.f, 0};
-  return by_types(a, [&](auto* pl, auto* pg, auto* pi) {
+  const Labels y{labels, a.label_type == IDX_I64, a.V};
+  return by_types(a, [&](auto* pl, auto* pg, auto same) {
     using TL = std::remove_pointer_t<decltype(pl)>;
     using TG = std::remove_pointer_t<decltype(pg)>;
-    using TI = std::remove_pointer_t<decltype(pi)>;
     constexpr int VW = 16 / sizeof(TL);
-    const uint64_t parts = ((a.V + 2 * (VW - 1)) / VW + kPart - 1) / kPart, blocks = parts * a.T;
+    const uint64_t parts = a.V < VW ? 1 : (a.V / VW + kPart - 1) / kPart, blocks = parts * a.T;
     if (blocks > 0x7fffffffu) return (int)hipErrorInvalidValue;
-    hipLaunchKernelGGL((loss_bwd_kernel<TL, TG, TI>), dim3((unsigned)blocks), dim3(256), 0, st, (const TL*)logits, (const TI*)labels, a.V, a.V_pad, a.ld, a.ld_grad, c, lse, dloss,
+    hipLaunchKernelGGL((loss_bwd_kernel<TL, TG, decltype(same)::value>), dim3((unsigned)blocks), dim3(256), 0, st, (const TL*)logits, y, a.V, a.V_pad, a.ld, a.ld_grad, c, lse, dloss,
                        (TG*)dlogits, (unsigned)parts);
     return last_err();
   });
