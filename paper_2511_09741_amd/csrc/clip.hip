@@ -10,13 +10,13 @@ namespace taw {
 
 // Tensors travel as kernel arguments, so a call copies nothing to the device and can be captured; a longer list takes several launches.
 constexpr int kListMax = 120;
-constexpr int kPiece = 16384;                 // elements of a tensor that a workgroup takes at a time
 struct TensorList {
   void* data[kListMax];
   unsigned long long n[kListMax];
   unsigned first[kListMax + 1];               // piece number of the tensor's first piece
   unsigned char bf16[kListMax];
   int count;
+  int piece;                                  // elements of a tensor that a workgroup takes at a time
 };
 
 __device__ __forceinline__ int tensor_of(const TensorList& l, unsigned piece) {
@@ -50,24 +50,57 @@ __device__ __forceinline__ double block_sum_f64(double x) {
 
 // =============================================================================== sum of squares
 // Squares and sums in fp64: an fp32 square overflows from 1.8e19 on, and the fp64 units keep up with memory.
+// A piece that is whole is read with 8 vectors in flight a thread.
 template <typename T>
 __device__ __forceinline__ double piece_sumsq(const T* __restrict__ p, int m) {
-  double s = 0.0;
-  for (int i = threadIdx.x; i < m; i += 256) {
-    const double v = (double)(float)p[i];
-    s = fma(v, v, s);
+  constexpr int VW = VecWidth<T>::value, U = 8;
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  const auto add = [&](const Vec<T, VW>& x) {
+#pragma unroll
+    for (int j = 0; j < VW; ++j) {
+      const double v = (double)x.get(j);
+      s[j & 3] = fma(v, v, s[j & 3]);
+    }
+  };
+  const int nv = m / VW;
+  int i = threadIdx.x;
+  for (; i + (U - 1) * 256 < nv; i += U * 256) {
+    Vec<T, VW> x[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) x[k].load_nt(p + (size_t)(i + k * 256) * VW);
+#pragma unroll
+    for (int k = 0; k < U; ++k) add(x[k]);
   }
-  return s;
+#pragma unroll 2
+  for (; i < nv; i += 256) {
+    Vec<T, VW> x;
+    x.load_nt(p + (size_t)i * VW);
+    add(x);
+  }
+  const int e = nv * VW + threadIdx.x;
+  if (e < m) {
+    const double v = (double)(float)p[e];
+    s[0] = fma(v, v, s[0]);
+  }
+  return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+// f(data, elements) for the pieces of this workgroup; data points to float or bf16
+template <typename F>
+__device__ __forceinline__ void over_pieces(const TensorList& l, F f) {
+  const unsigned pieces = l.first[l.count];
+  for (unsigned piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+    const int t = tensor_of(l, piece);
+    const unsigned long long at = (unsigned long long)(piece - l.first[t]) * l.piece;
+    const int m = (int)(l.n[t] - at < l.piece ? l.n[t] - at : l.piece);
+    if (l.bf16[t]) f((bf16_t*)l.data[t] + at, m);
+    else f((float*)l.data[t] + at, m);
+  }
 }
 
 __global__ void __launch_bounds__(256) sumsq_kernel(const TensorList l, double* __restrict__ partials) {
   double s = 0.0;
-  for (unsigned piece = blockIdx.x; piece < l.first[l.count]; piece += gridDim.x) {
-    const int t = tensor_of(l, piece);
-    const unsigned long long at = (unsigned long long)(piece - l.first[t]) * kPiece;
-    const int m = (int)(l.n[t] - at < kPiece ? l.n[t] - at : kPiece);
-    s += l.bf16[t] ? piece_sumsq((const bf16_t*)l.data[t] + at, m) : piece_sumsq((const float*)l.data[t] + at, m);
-  }
+  over_pieces(l, [&](const auto* p, int m) { s += piece_sumsq(p, m); });
   s = block_sum_f64<4>(s);
   if (threadIdx.x == 0) partials[blockIdx.x] = s;
 }
@@ -99,36 +132,61 @@ __global__ void __launch_bounds__(64) clip_coef_kernel(float max_norm, float gra
 // =============================================================================== scaling in place
 template <typename T>
 __device__ __forceinline__ void piece_scale(T* __restrict__ p, int m, float c) {
-  for (int i = threadIdx.x; i < m; i += 256) p[i] = (T)((float)p[i] * c);
+  constexpr int VW = VecWidth<T>::value, U = 4;
+  const auto scaled = [&](const Vec<T, VW>& x) {
+    Vec<T, VW> o;
+#pragma unroll
+    for (int j = 0; j < VW; ++j) o.set(j, x.get(j) * c);
+    return o;
+  };
+  const int nv = m / VW;
+  int i = threadIdx.x;
+  for (; i + (U - 1) * 256 < nv; i += U * 256) {
+    Vec<T, VW> x[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) x[k].load_nt(p + (size_t)(i + k * 256) * VW);
+#pragma unroll
+    for (int k = 0; k < U; ++k) scaled(x[k]).store_nt(p + (size_t)(i + k * 256) * VW);
+  }
+#pragma unroll 2
+  for (; i < nv; i += 256) {
+    Vec<T, VW> x;
+    x.load_nt(p + (size_t)i * VW);
+    scaled(x).store_nt(p + (size_t)i * VW);
+  }
+  const int e = nv * VW + threadIdx.x;
+  if (e < m) p[e] = (T)((float)p[e] * c);
 }
 
 __global__ void __launch_bounds__(256) clip_kernel(const TensorList l, const taw_clip_state* __restrict__ state) {
   const float c = state->coef;
   if (c == 1.f || state->nonfinite) return;
-  for (unsigned piece = blockIdx.x; piece < l.first[l.count]; piece += gridDim.x) {
-    const int t = tensor_of(l, piece);
-    const unsigned long long at = (unsigned long long)(piece - l.first[t]) * kPiece;
-    const int m = (int)(l.n[t] - at < kPiece ? l.n[t] - at : kPiece);
-    if (l.bf16[t]) piece_scale((bf16_t*)l.data[t] + at, m, c);
-    else piece_scale((float*)l.data[t] + at, m, c);
-  }
+  over_pieces(l, [&](auto* p, int m) { piece_scale(p, m, c); });
 }
 
 // =============================================================================== launchers
 static inline int last_err() { return (int)hipGetLastError(); }
 
 constexpr unsigned kGridMax = 2048;
+// Pieces of 16384 elements keep 8 vectors in flight a thread; where they are too few for the chip, pieces of 2048.
+static int piece_of(const taw_tensor* t, int count) {
+  size_t n = 0;
+  for (int i = 0; i < count; ++i) n += t[i].n;
+  return n < ((size_t)1 << 22) ? 2048 : 16384;
+}
+
 // cuts the list into launches; f(list, grid) returns a status
 template <typename F>
 static int over_list(const taw_tensor* t, int count, F f) {
   TensorList l;
+  l.piece = piece_of(t, count);
   int i = 0;
   while (i < count) {
     l.count = 0;
     unsigned pieces = 0;
     for (; i < count && l.count < kListMax; ++i) {
       if (!t[i].n) continue;
-      const unsigned long long np = (t[i].n + kPiece - 1) / kPiece;
+      const unsigned long long np = (t[i].n + l.piece - 1) / l.piece;
       if (np > 0x7fffffffull) return (int)hipErrorInvalidValue;
       if (pieces + np > 0x7fffffffull) break;
       l.data[l.count] = t[i].data;
