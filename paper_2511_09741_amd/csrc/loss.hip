@@ -152,14 +152,14 @@ __device__ __forceinline__ void gradient(const R& row, unsigned c, const typenam
   row.store(c, g);
 }
 
-// what a row comes to, from its maximum m, its sum of exponentials and (label smoothing) its sum of logits; thread 0 stores it
+// what a row comes to, from its maximum m, its sum of exponentials and (label smoothing) its sum of logits; the thread that is told to stores it
 struct RowResult {
   float scale, share, own;                         // gradient: scale * exp(l) - share, - own at the label
-  __device__ __forceinline__ RowResult(const Shift& sh, float m, float sum, float total, float ly, int V, const RowTerms& c, float counted, int64_t t,
+  __device__ __forceinline__ RowResult(const Shift& sh, float m, float sum, float total, float ly, int V, const RowTerms& c, float counted, int64_t t, bool store,
                                        float* __restrict__ rows, float* __restrict__ lse_out) {
     const bool none = sum == 0.f;                  // nothing but -inf
     const float lse = none ? -kInf : sh.lse(m, sum);
-    if (threadIdx.x == 0) {
+    if (store) {
       float r = none ? kInf : lse - (1.f - c.eps) * ly;
       if (c.eps != 0.f) r -= c.eps / (float)V * total;
       if (c.z != 0.f) r += c.z * lse * lse;
@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(NT) loss_row_kernel(const TL* logits, const La
     if (k < n) sum_exp<R>(x[k], sh, sum);
   }
   sum = block_sum<NW>(sum, red);
-  const RowResult g(sh, m, sum, total, ly, V, c, counted, t, rows, lse_out);
+  const RowResult g(sh, m, sum, total, ly, V, c, counted, t, tid == 0, rows, lse_out);
   if (!GRAD) return;
 #pragma unroll
   for (int k = 0; k < MAXC; ++k) {
@@ -392,10 +392,149 @@ __global__ void __launch_bounds__(256) loss_bwd_kernel(const TL* logits, const L
   for (int v = V + threadIdx.x; v < V_pad; v += 256) dlogits[t * ld_grad + v] = (TG)0.f;
 }
 
+// =============================================================================== few rows
+// A few rows that are more than a workgroup holds: each is cut into `parts` runs of at most kSplitVecs vectors, a workgroup on each, which leaves the run's
+// maximum, sum of exponentials and sum of logits; whoever needs the row's joins those of its parts, in order.  With a gradient the logits are read
+// twice, the second time from the memory-side cache.  131072 classes, us without and with the cut: gradient from bf16, 1 row 20 and 10, 128 rows 25 and 20,
+// 333 rows 48 and 43, 512 rows 59 and 64; from fp32, 1 row 23 and 10, 128 rows 32 and 28, 200 rows 39 and 42; the loss alone of fp32, 1 row 14 and 7, 32 rows
+// 18 and 11, 128 rows 19 and 25 (one workgroup joins them all).  A row that a workgroup does hold gains nothing (50001 classes of bf16, 1 row 11.1 and
+// 11.2, 333 rows 21 and 23).
+constexpr int kSplitVecs = 2048, kSplitMax = 64, kSplitRows = 128, kSplitRowsAlone = 64;
+struct PartSum {
+  float m, sum, total, ly;                         // ly: the logit at the label, in part 0 (dlogits may take the logits' place before a row is joined)
+};
+
+template <typename TL>
+__global__ void __launch_bounds__(256) loss_part_kernel(const TL* __restrict__ logits, const Labels labels, int V, int64_t ld, float eps, int len, unsigned parts,
+                                                        PartSum* __restrict__ out) {
+  typedef RowVecs<TL, TL, true> R;
+  constexpr int NT = 256, U = kSplitVecs / NT, NW = NT / 64;
+  __shared__ float red[NW];
+  const int64_t t = blockIdx.x / parts;
+  const int part = (int)(blockIdx.x - (unsigned)t * parts), y = labels[t], tid = threadIdx.x;
+  if (y < 0) return;
+  const R row(logits, nullptr, t, V, ld, ld);
+  const int from = part * len, left = row.count - from, m_ = left < len ? left : len, n = m_ > tid ? (m_ - tid + NT - 1) / NT : 0;
+  typename R::vec_t x[U];
+  if (m_ > 0)
+#pragma unroll
+    for (int k = 0; k < U; ++k) row.template load<true>(from + (k < n ? tid + k * NT : m_ - 1), x[k]);
+  float top = -kInf, total = 0.f, sum = 0.f, edge = -kInf;
+  int e;
+  if (part == 0 && row.edge(&e)) {
+    top = edge = (float)row.in[e];
+    total = edge;
+  }
+#pragma unroll
+  for (int k = 0; k < U; ++k)
+    if (k < n)
+#pragma unroll
+      for (int j = 0; j < R::VW; ++j) top = fmaxf(top, x[k].get(j));
+  top = block_max<NW>(top, red);
+  const Shift sh(top == -kInf ? 0.f : top);
+  sum = sh.exp(edge);
+#pragma unroll
+  for (int k = 0; k < U; ++k) {
+    x[k].pin();
+    if (k < n)
+#pragma unroll
+      for (int j = 0; j < R::VW; ++j) {
+        sum += sh.exp(x[k].get(j));
+        if (eps != 0.f) total += x[k].get(j);
+      }
+  }
+  sum = block_sum<NW>(sum, red);
+  if (eps != 0.f) total = block_sum<NW>(total, red);
+  if (tid == 0) out[blockIdx.x] = PartSum{top, sum, total, part == 0 ? (float)logits[t * ld + y] : 0.f};
+}
+
+// what a part's sum counts for beside the row's maximum m
+__device__ __forceinline__ float part_weight(const PartSum& p, float m) {
+  if (p.m == -kInf) return 0.f;
+  const Shift a(p.m), b(m);
+  return p.m == m ? 1.f : a.huge != b.huge ? (p.m > m ? kInf : 0.f) : __builtin_amdgcn_exp2f(a.ms - b.ms);
+}
+
+// joined by a wavefront, a part a lane: every lane has the result
+__device__ __forceinline__ PartSum join_parts(const PartSum* __restrict__ p, int parts) {
+  const int lane = threadIdx.x & 63;
+  PartSum mine = lane < parts ? p[lane] : PartSum{-kInf, 0.f, 0.f, 0.f}, all;
+  all.m = wave_max(mine.m);
+  all.sum = wave_sum(mine.sum * part_weight(mine, all.m));
+  all.total = wave_sum(mine.total);
+  all.ly = __shfl(mine.ly, 0, 64);
+  return all;
+}
+
+// the gradient of a part, from the sums of all of its row's
+template <typename TL, typename TG, bool SAME>
+__global__ void __launch_bounds__(256) loss_part_grad_kernel(const TL* logits, const Labels labels, int T_, int V, int V_pad, int64_t ld, int64_t ld_grad, RowTerms c, int len,
+                                                             unsigned parts, const PartSum* __restrict__ sums, float* __restrict__ rows, float* __restrict__ lse_out,
+                                                             TG* dlogits) {
+  typedef RowVecs<TL, TG, SAME> R;
+  constexpr int NT = 256, U = kSplitVecs / NT, NW = NT / 64;
+  __shared__ float red[NW];
+  const int64_t t = blockIdx.x / parts;
+  const int part = (int)(blockIdx.x - (unsigned)t * parts), y = labels[t], tid = threadIdx.x;
+  const R row(logits, dlogits, t, V, ld, ld_grad);
+  const int from = part * len, left = row.count - from, m_ = left < len ? left : len, n = m_ > tid ? (m_ - tid + NT - 1) / NT : 0;
+  int e;
+  const bool edge = part == 0 && row.edge(&e);
+  if (y < 0) {
+    const float zero[R::VW] = {};
+    for (int k = 0; k < n; ++k) row.store(from + tid + k * NT, zero);
+    if (edge) row.out[e] = (TG)0.f;
+    if (part == 0 && tid == 0) {
+      rows[t] = 0.f;
+      if (lse_out) lse_out[t] = 0.f;
+    }
+  } else {
+    typename R::vec_t x[U];
+    if (m_ > 0)
+#pragma unroll
+      for (int k = 0; k < U; ++k) row.load(from + (k < n ? tid + k * NT : m_ - 1), x[k]);
+    const float le = edge ? (float)row.in[e] : 0.f;
+    const PartSum all = join_parts(sums + t * parts, (int)parts);
+    float counted = 1.f;
+    if (c.mean) {
+      int k = 0;
+      for (int i = tid; i < T_; i += NT) k += labels[i] >= 0;
+      counted = block_sum<NW>((float)k, red);
+    }
+    const float m = all.m == -kInf ? 0.f : all.m;
+    const Shift sh(m);
+    const RowResult g(sh, m, all.sum, all.total, all.ly, V, c, counted, t, part == 0 && tid == 0, rows, lse_out);
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (k < n) gradient<false>(row, from + tid + k * NT, x[k], sh, g.scale, g.share, g.own, y);
+    if (edge) row.out[e] = __builtin_fmaf(g.scale, sh.exp(le), -g.share) - (e + row.head == y ? g.own : 0.f);
+  }
+  if (part == 0)
+    for (int v = V + tid; v < V_pad; v += NT) dlogits[t * ld_grad + v] = (TG)0.f;
+}
+
 // =============================================================================== sum of the rows' losses
-__global__ void __launch_bounds__(1024) loss_sum_kernel(const float* __restrict__ rows, const Labels labels, int T_, int mean, float* __restrict__ loss) {
+// parts != 0: the rows' losses are formed here, from the sums of their parts, a wavefront on each
+__global__ void __launch_bounds__(1024) loss_sum_kernel(float* rows, const Labels labels, int T_, int mean, float* __restrict__ loss, int parts, const PartSum* __restrict__ sums, int V,
+                                                        RowTerms c, float* __restrict__ lse_out) {
   __shared__ double red[16];
   __shared__ int redn[16];
+  if (parts) {
+    const bool first = (threadIdx.x & 63) == 0;
+    for (int t = threadIdx.x >> 6; t < T_; t += 16) {
+      if (labels[t] < 0) {
+        if (first) {
+          rows[t] = 0.f;
+          if (lse_out) lse_out[t] = 0.f;
+        }
+        continue;
+      }
+      const PartSum all = join_parts(sums + (size_t)t * parts, parts);
+      const float m = all.m == -kInf ? 0.f : all.m;
+      const RowResult g(Shift(m), m, all.sum, all.total, all.ly, V, c, 1.f, t, first, rows, lse_out);
+    }
+    __syncthreads();
+  }
   double s = 0.0;
   int n = 0;
   for (int t = threadIdx.x; t < T_; t += 1024) {
@@ -426,7 +565,22 @@ __global__ void __launch_bounds__(1024) loss_sum_kernel(const float* __restrict_
 // =============================================================================== launchers
 static inline int last_err() { return (int)hipGetLastError(); }
 
-size_t loss_workspace_bytes(int T_) { return 256 + ((size_t)T_ * 4 + 255) / 256 * 256; }      // the count; the rows' losses where the caller has no use for them
+constexpr int kHeldVecs = 512 * 16;      // of a row, at most, by a workgroup
+
+// parts that a row is cut into, 0: not cut
+static int parts_of(const LossArgs& a, bool grad) {
+  const int64_t vecs = a.V / (a.dtype == DT_BF16 ? 8 : 4);
+  if (!a.T || a.T > (grad ? kSplitRows : kSplitRowsAlone) || vecs <= kHeldVecs) return 0;
+  const int64_t least = (vecs + kSplitVecs - 1) / kSplitVecs, want = 1024 / a.T, most = vecs / 512;
+  const int64_t parts = want < least ? least : want < most ? want : most;
+  return least > kSplitMax ? 0 : parts < kSplitMax ? (int)parts : kSplitMax;
+}
+
+// the count; the rows' losses where the caller has no use for them; the sums of parts
+static size_t rows_bytes(int T_) { return ((size_t)T_ * 4 + 255) / 256 * 256; }
+size_t loss_workspace_bytes(const LossArgs& a) {
+  return 256 + rows_bytes(a.T) + (size_t)a.T * parts_of(a, true) * sizeof(PartSum);
+}
 
 template <typename F>
 static int by_types(const LossArgs& a, F f) {
@@ -453,9 +607,21 @@ int launch_loss(const LossArgs& a, const void* logits, const void* labels, float
     constexpr bool SAME = decltype(same)::value;
     const TL* l = (const TL*)logits;
     TG* d = (TG*)dlogits;
-    if (a.T) {
-      constexpr int VW = 16 / sizeof(TL);
-      const int vecs = a.V / VW;
+    constexpr int VW = 16 / sizeof(TL);
+    const int vecs = a.V / VW, parts = parts_of(a, d != nullptr);
+    PartSum* sums = (PartSum*)((char*)ws + 256 + rows_bytes(a.T));
+    if (parts) {
+      const int len = (vecs + parts - 1) / parts;
+      hipLaunchKernelGGL((loss_part_kernel<TL>), dim3((unsigned)(a.T * parts)), dim3(256), 0, st, l, y, a.V, a.ld, a.eps, len, (unsigned)parts, sums);
+      int e = last_err();
+      if (e) return e;
+      if (d) {
+        hipLaunchKernelGGL((loss_part_grad_kernel<TL, TG, SAME>), dim3((unsigned)(a.T * parts)), dim3(256), 0, st, l, y, a.T, a.V, a.V_pad, a.ld, a.ld_grad, c, len, (unsigned)parts,
+                           sums, rows, lse, d);
+        e = last_err();
+        if (e) return e;
+      }
+    } else if (a.T) {
       if (d && a.mean && a.T > kCountedInline) hipLaunchKernelGGL(loss_count_kernel, dim3(1), dim3(1024), 0, st, y, a.T, count);
       else count = nullptr;
 #define TAW_LOSS(NT, MAXC, MORE)                                                                                                                    \
@@ -466,13 +632,13 @@ int launch_loss(const LossArgs& a, const void* logits, const void* labels, float
       if (vecs <= 64 * 8) TAW_LOSS(64, 8, false);
       else if (vecs <= 256 * 8) TAW_LOSS(256, 8, false);
       else if (vecs <= 512 * 8) TAW_LOSS(512, 8, false);
-      else if (vecs <= 512 * 16) TAW_LOSS(512, 16, false);
+      else if (vecs <= kHeldVecs) TAW_LOSS(512, 16, false);
       else TAW_LOSS(512, 16, true);
 #undef TAW_LOSS
       const int e = last_err();
       if (e) return e;
     }
-    hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, st, rows, y, a.T, a.mean, loss);
+    hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, st, rows, y, a.T, a.mean, loss, d ? 0 : parts, sums, a.V, c, lse);
     return last_err();
   });
 }

@@ -114,7 +114,7 @@ static int check_dlogits(const LossArgs& a, const void* logits, const void* dlog
 
 extern "C" size_t taw_loss_workspace_bytes(const taw_loss_desc* desc) {
   LossArgs a;
-  return check_loss(desc, &a) ? 0 : loss_workspace_bytes(a.T);
+  return check_loss(desc, &a) ? 0 : loss_workspace_bytes(a);
 }
 
 static int loss_call(const taw_loss_desc* desc, const void* logits, const void* labels, int32_t label_type, float* loss, float* loss_rows, float* lse,
@@ -135,7 +135,7 @@ static int loss_call(const taw_loss_desc* desc, const void* logits, const void* 
   }
   TAW_REQUIRE_PTR(loss); TAW_REQUIRE_PTR(workspace);
   TAW_REQUIRE_ALIGNED(loss); TAW_REQUIRE_ALIGNED(workspace); TAW_REQUIRE_ALIGNED(loss_rows); TAW_REQUIRE_ALIGNED(lse);
-  if (workspace_bytes < loss_workspace_bytes(a.T)) return fail(TAW_ERR_WORKSPACE, "workspace_bytes=%zu < required %zu", workspace_bytes, loss_workspace_bytes(a.T));
+  if (workspace_bytes < loss_workspace_bytes(a)) return fail(TAW_ERR_WORKSPACE, "workspace_bytes=%zu < required %zu", workspace_bytes, loss_workspace_bytes(a));
   TAW_LAUNCH(launch_loss(a, logits, labels, loss, loss_rows, lse, grad ? dlogits : nullptr, workspace, (hipStream_t)stream), "loss");
   return TAW_OK;
 }

@@ -211,7 +211,7 @@ struct LossArgs {
   float eps, z, grad_scale;
   int mean;
 };
-size_t loss_workspace_bytes(int T);
+size_t loss_workspace_bytes(const LossArgs& a);
 // dlogits == nullptr: the loss alone.  rows, lse may be nullptr
 int launch_loss(const LossArgs& a, const void* logits, const void* labels, float* loss, float* rows, float* lse, void* dlogits, void* ws, hipStream_t st);
 int launch_loss_bwd(const LossArgs& a, const void* logits, const void* labels, const float* lse, const float* dloss, void* dlogits, hipStream_t st);

@@ -226,7 +226,7 @@ def check_loss(taw, T, V, dtype, grad, ldt, eps=0.0, z=0.0, mean=True, pad=0, od
 
 
 TYPES = [("bf16", "bf16", "i64"), ("f32", "bf16", "i32"), ("f32", "f32", "i64")]
-LOSS = [(1, 1), (1, 2), (3, 5), (5, 63), (7, 64), (4, 1000), (300, 257), (2, 2047), (3, 4097), (2, 8200), (2, 16391), (2, 32003), (2, 50001), (2, 65537), (2, 131073), (1, 262144)]
+LOSS = [(1, 1), (1, 2), (3, 5), (5, 63), (7, 64), (4, 1000), (300, 257), (2, 2047), (3, 4097), (2, 8200), (2, 16391), (2, 32003), (2, 50001), (2, 65537), (2, 131073), (1, 262144), (129, 66000), (3, 600011)]
 
 
 @pytest.mark.parametrize("T,V", LOSS)
