@@ -1,7 +1,7 @@
 #!/usr/bin/env python3
 """Benchmark of the decoder-layer hot path on one MI355X.
 
-    python bench.py [--gpus 1] [--steps K] [--warmup W] [--workload default|C2|C3|C4|C5|P-<H>-<S>|paper-sweep|diag]
+    python bench.py [--gpus 1] [--steps K] [--warmup W] [--workload default|C2|C3|C4|C5|P-<H>-<S>|paper-sweep|model|diag]
 
 One step = one pass of the whole hot path over one micro-batch of synthetic input:
   taw_weight_stage   the other layer's weight chunk is copied owner-store -> staging buffer on a
@@ -21,7 +21,8 @@ configuration C3 (S = 32768) at the top level of the JSON line and C2 (S = 8192)
 with its own step time, fraction of the bf16 MFMA peak and roofline of its dominant kernel.
 C4 runs four distinct layers (forward 0..3, backward 3..0, every chunk arriving through the staging
 buffers); C5 runs four micro-batches through one layer, accumulating into one fp32 shard while the
-next layer's chunk is staged; paper-sweep runs the nine shapes of the paper's throughput table.
+next layer's chunk is staged; paper-sweep runs the nine shapes of the paper's throughput table; model runs a whole training
+step of a four-layer model: embedding, layers, last norm, head, loss, all of it backward, gradient norm, clipped AdamW.
 
 Steps are timed with HIP events on the compute stream (one per step boundary): the K timed steps sit
 between a synchronisation on both sides, `ms_per_step` is their mean, median and minimum are beside it.
@@ -57,6 +58,7 @@ if ROOT not in sys.path:
 
 PEAK_BF16_TFLOPS = 2500.0   # MI355X dense bf16 MFMA
 PEAK_HBM_GBS = 8000.0
+MODEL_VOCAB = 32000         # of --workload model
 # HBM-side bytes per launch of the dominant kernel from two rocprofv3 --pmc runs of this file (FETCH_SIZE, WRITE_SIZE; each
 # scaled by what the counter reads for the staging copy kernel, a plain copy of known size).  Precomputed: a counter run is a
 # separate profiler invocation, not part of a timed run.  (workload, kernel) -> (bytes, file under profiles/ it comes from)
@@ -665,6 +667,107 @@ def cpu_baseline(env):
                       "C3 has four times the tokens at four times the attention length, where the oracle's rate is no higher"}
 
 
+# =============================================================================== a training step of a small model
+def run_model(env, cfg, steps, warmup):
+    """Token ids in, updated weights out: taw_embed_fwd, the layers, the last norm, the head's logits (fp32, as the product's
+    accumulators hold them), taw_loss_fwd_bwd, all of it backward, taw_grad_norm over every shard and taw_optimizer_step_clipped
+    shard by shard, with no host synchronisation anywhere."""
+    torch, taw, I = env.torch, env.taw, env.I
+    compute = torch.cuda.current_stream()
+    T, H, V, nl = cfg.B * cfg.S, cfg.H, MODEL_VOCAB, cfg.n_layers
+    desc = taw.desc_from_config(cfg)
+    P = taw.taw_layer_weight_layout(desc)["total_elems"]
+    bf, f32 = torch.bfloat16, torch.float32
+
+    def empty(shape, dtype=bf):
+        return torch.empty(shape, dtype=dtype, device="cuda")
+
+    lay = taw.taw_layer_weight_layout(desc)
+    chunks = []
+    for l in range(nl):
+        c = I.device_normal((P,), seed=300 + l, std=cfg.sigma_w, dtype=bf)
+        for g in ("gamma_attn", "gamma_mlp"):
+            c[lay[g]:lay[g] + H] = 1.0
+        chunks.append(c)
+    chunks += [I.device_normal((V * H,), seed=400, std=1.0, dtype=bf), I.device_normal((V * H,), seed=401, std=cfg.sigma_w, dtype=bf),
+               torch.ones(H, dtype=bf, device="cuda")]
+    emb, head, gamma = chunks[nl], chunks[nl + 1], chunks[nl + 2]
+    masters = [c.float() for c in chunks]
+    m, v = [torch.zeros_like(w) for w in masters], [torch.zeros_like(w) for w in masters]
+    G = [torch.zeros_like(w) for w in masters]
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(500)
+    ids = torch.randint(0, V, (T,), generator=gen, device="cuda", dtype=torch.int32)
+    labels = torch.cat([ids[1:], ids.new_full((1,), -100)])
+    acts = [empty((T, H)) for _ in range(nl + 1)]
+    grads = [empty((T, H)) for _ in range(2)]
+    ctx = [empty((taw.taw_layer_ctx_bytes(desc),), torch.uint8) for _ in range(nl)]
+    ws_bytes = taw.taw_layer_workspace_bytes(desc)
+    ws = empty((ws_bytes,), torch.uint8)
+    rope = empty((cfg.S * (cfg.head_dim // 2) * 2,), f32)
+    taw.taw_rope_table_init(desc, rope)
+    xn, r, logits, dlogits, dxn = empty((T, H)), empty((T,), f32), empty((T, V), f32), empty((T, V)), empty((T, H))
+    ed = taw.make_embed_desc(taw.TAW_BF16, T, H, V)
+    ld = taw.make_loss_desc(taw.TAW_F32, T, V, grad_dtype=taw.TAW_BF16)
+    lst, state, loss = taw.make_tensor_list(G), taw.new_clip_state(), empty((2,), f32)
+    ws_e, ws_l = empty((max(16, taw.taw_embed_bwd_workspace_bytes(ed)),), torch.uint8), empty((taw.taw_loss_workspace_bytes(ld),), torch.uint8)
+    ws_n, ws_g = empty((taw.taw_grad_norm_workspace_bytes(lst),), torch.uint8), empty((taw.taw_op_rmsnorm_bwd_scratch_floats(H),), f32)
+    ws_h = empty((max(4, taw.taw_op_linear_bwd_scratch_floats(T, V, H)),), f32)
+    done = [0]
+
+    def step(mark=lambda name: None):
+        done[0] += 1
+        mark("start")
+        taw.taw_embed_fwd(ed, ids, emb, acts[0], compute)
+        mark("embed_fwd")
+        for l in range(nl):
+            taw.taw_layer_fwd(desc, chunks[l], rope, acts[l], acts[l + 1], ctx[l], ws, ws_bytes, compute)
+        mark("layers_fwd")
+        taw.taw_op_rmsnorm_fwd(taw.TAW_BF16, T, H, acts[nl], gamma, cfg.rms_eps, xn, r, compute)
+        taw.taw_op_gemm(taw.TAW_BF16, taw.TAW_GEMM_NT, T, V, H, xn, H, head, H, logits, V, taw.TAW_F32, stream=compute)
+        mark("norm_and_head_fwd")
+        taw.taw_loss_fwd_bwd(ld, logits, labels, loss, None, None, dlogits, ws_l, stream=compute)
+        mark("loss_fwd_bwd")
+        taw.taw_op_linear_bwd(taw.TAW_BF16, T, V, H, dlogits, head, xn, dxn, G[nl + 1], stream=compute, scratch=ws_h)
+        taw.taw_op_rmsnorm_bwd(taw.TAW_BF16, T, H, dxn, acts[nl], r, gamma, None, grads[nl & 1], G[nl + 2], 0, ws_g, compute)
+        mark("head_and_norm_bwd")
+        for l in reversed(range(nl)):
+            taw.taw_layer_bwd(desc, chunks[l], rope, acts[l], grads[(l + 1) & 1], ctx[l], grads[l & 1], G[l], ws, ws_bytes, compute)
+        mark("layers_bwd")
+        taw.taw_embed_bwd(ed, ids, grads[0], G[nl], ws_e, stream=compute)
+        mark("embed_bwd")
+        taw.taw_grad_norm(lst, 1.0, 1.0, state, ws_n, stream=compute)
+        mark("grad_norm")
+        for i in range(len(chunks)):
+            taw.taw_optimizer_step_clipped(state, chunks[i], taw.TAW_BF16, masters[i], m[i], v[i], G[i], G[i].numel(), done[0], lr=3e-4, beta1=0.9,
+                                           beta2=0.95, weight_decay=0.1, stream=compute)
+        mark("optimizer")
+
+    for _ in range(max(1, warmup)):
+        step()
+    first_loss = float(loss[0])
+    st = _stats(env.timed_steps(step, steps))
+    last_loss = float(loss[0])
+    marks = []
+
+    def record(name):
+        marks.append((name, torch.cuda.Event(enable_timing=True)))
+        marks[-1][1].record(compute)
+
+    step(record)
+    torch.cuda.synchronize()
+    parts = {b[0]: round(a[1].elapsed_time(b[1]), 4) for a, b in zip(marks, marks[1:])}
+    gemm_fl, attn_fl = model_flops(cfg)
+    flops = (gemm_fl + attn_fl) * nl + 6.0 * T * V * H
+    value = flops / st["mean"] / 1e9
+    return {"name": cfg.name, "ms_per_step": round(st["mean"], 4), "ms_per_step_median": round(st["median"], 4), "ms_per_step_min": round(st["min"], 4),
+            "value": round(value, 2), "frac_of_bf16_mfma_peak": round(value / PEAK_BF16_TFLOPS, 4), "model_flops_per_step": flops,
+            "workload": f"{cfg.name}: training step of {nl} bf16 decoder layers, B={cfg.B} S={cfg.S} H={cfg.H} heads={cfg.n_heads}x{cfg.head_dim} I={cfg.I}, "
+                        f"embedding and head of {V} rows, cross entropy, global norm clipping, AdamW",
+            "model": {"ms_of_one_step": parts, "tokens_per_s": round(T / st["mean"] * 1e3, 1), "loss_before": round(first_loss, 4), "loss_after": round(last_loss, 4),
+                      "grad_norm": round(float(state.norm), 4), "clip_coef": round(float(state.coef), 6)}}
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -672,7 +775,7 @@ def main():
     ap.add_argument("--warmup", type=int, default=3)
     ap.add_argument("--workload", default="default",
                     help="default (C3 at the top level and C2 beside it), C2, C3, C4, C5, a shape of the paper's throughput table as "
-                         "P-<H>-<S> (H in 1024/2048/4096, S in 4096/8192/16384; micro-batch size as in that table), or paper-sweep (all nine)")
+                         "P-<H>-<S> (H in 1024/2048/4096, S in 4096/8192/16384; micro-batch size as in that table), paper-sweep (all nine), or model")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-kernel-leg", action="store_true")
     ap.add_argument("--no-recompute-leg", action="store_true")
@@ -702,6 +805,9 @@ def main():
         top = run_c4(env, I.CONFIGS["C4"], args.steps, args.warmup)
     elif wl == "C5":
         top = run_c5(env, I.CONFIGS["C5"], args.steps, args.warmup)
+    elif wl == "model":
+        top = run_model(env, I.LayerConfig("model", I.BF16, 4, 4096, 2048, 16, 128, 5632, n_layers=4), args.steps, args.warmup)
+        extra["model"] = top["model"]
     elif wl == "paper-sweep":
         rows = []
         for h_ in (1024, 2048, 4096):
@@ -739,6 +845,8 @@ def main():
     cpu = None if args.no_cpu_baseline else cpu_baseline(env)
 
     metric = "layer fwd+bwd TFLOP/s (model FLOPs; fraction of the bf16 MFMA peak in config)"
+    if wl == "model":
+        metric = "training step TFLOP/s (model FLOPs of layers and head; fraction of the bf16 MFMA peak in config)"
     if wl == "default":
         metric += ", H=4096: S=32768 (C3) at the top level, S=8192 (C2) under c2"
     out = {
