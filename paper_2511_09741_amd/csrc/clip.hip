@@ -111,6 +111,7 @@ __device__ __forceinline__ void finish_clip(double sumsq, float max_norm, float 
   state->norm = norm;
   state->coef = !fine ? 0.f : norm > max_norm ? max_norm / norm : 1.f;
   state->nonfinite = fine ? 0 : 1;
+  for (int i = 0; i < 3; ++i) state->reserved[i] = 0;
 }
 
 __global__ void __launch_bounds__(256) sumsq_finish_kernel(const double* __restrict__ partials, int np, int set, int finish, float max_norm, float grad_scale,

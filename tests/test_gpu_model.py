@@ -512,3 +512,138 @@ def test_a_training_step(taw, cfg, V):
     assert U.tensor_scale_err(f64(m), 0.1 * coef * ref["embed"].reshape(-1)) <= 2 * tol and not Ge.any()
     unnamed = np.setdiff1d(np.arange(V), ids)
     assert np.allclose(f64(master).reshape(V, H)[unnamed], w0.reshape(V, H)[unnamed] * (1 - 1e-3), rtol=1e-6, atol=0)
+
+
+# ----------------------------------------------------------------------------- as a program uses them
+class Pieces:
+    """Every operation on buffers of its own, at sizes that take the kernels for many tokens (embedding: the sort) and for a few."""
+
+    def __init__(self, T, H, V, seed):
+        rng = np.random.default_rng(seed)
+        self.T, self.V = T, V
+        self.ids = on_gpu(zipf_ids(rng, T + 1, V), torch.int32)
+        self.labels = self.ids[1:]                       # the next token: aligned to its type, not to 16 bytes
+        self.ids = self.ids[:-1]
+        self.E, self.dx = on_gpu(rng.normal(size=(V, H)), torch.bfloat16), on_gpu(rng.normal(size=(T, H)), torch.bfloat16)
+        self.logits = on_gpu(rng.normal(0, 2, (T, V)), torch.float32)
+        self.ed, self.ld = taw.make_embed_desc(taw.TAW_BF16, T, H, V), taw.make_loss_desc(taw.TAW_F32, T, V, grad_dtype=taw.TAW_BF16)
+        self.x, self.G, self.dlogits = torch.empty_like(self.dx), torch.empty((V, H), device="cuda"), torch.empty((T, V), dtype=torch.bfloat16, device="cuda")
+        self.loss, self.lse = torch.empty(2, device="cuda"), torch.empty(T, device="cuda")
+        self.lst, self.state = taw.make_tensor_list([self.G]), taw.new_clip_state()
+        self.w, self.m, self.v, self.chunk = self.E.float(), torch.zeros_like(self.G), torch.zeros_like(self.G), self.E.clone()
+        self.ws = [scratch(n) for n in (taw.taw_embed_bwd_workspace_bytes(self.ed), taw.taw_loss_workspace_bytes(self.ld), taw.taw_grad_norm_workspace_bytes(self.lst))]
+        torch.cuda.synchronize()
+
+    def outs(self):
+        return [self.x, self.G, self.dlogits, self.loss, self.lse, self.state.buffer, self.w, self.m, self.v, self.chunk]
+
+    def run(self, stream):
+        taw.taw_embed_fwd(self.ed, self.ids, self.E, self.x, stream)
+        taw.taw_loss_fwd_bwd(self.ld, self.logits, self.labels, self.loss, None, self.lse, self.dlogits, self.ws[1], stream=stream)
+        taw.taw_embed_bwd(self.ed, self.ids, self.dx, self.G, self.ws[0], stream=stream)
+        taw.taw_grad_norm(self.lst, 1.0, 1.0, self.state, self.ws[2], stream=stream)
+        taw.taw_grad_clip(self.lst, self.state, stream)
+        taw.taw_optimizer_step_clipped(self.state, self.chunk, taw.TAW_BF16, self.w, self.m, self.v, self.G, self.G.numel(), step=1, stream=stream)
+
+    def reset(self):
+        self.w.copy_(self.E.float()), self.m.zero_(), self.v.zero_()
+
+
+@pytest.mark.parametrize("T,H,V", [(3000, 256, 1000), (100, 64, 70003)])
+def test_captured_and_replayed(taw, T, H, V):
+    """Recorded into a graph and replayed with other work between, every replay has the eager results' bits, also with new inputs in the same buffers."""
+    p = Pieces(T, H, V, 1)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            p.run(torch.cuda.current_stream())
+    for rep in range(4):
+        if rep == 2:
+            p.logits.mul_(0.5), p.dx.add_(1.0)
+            p.ids.copy_(torch.flip(p.ids, [0]))
+        p.reset()
+        torch.cuda.synchronize()
+        p.run(torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        want = [t.clone() for t in p.outs()]
+        for t in p.outs():
+            if t is not p.w and t is not p.m and t is not p.v:
+                t.view(torch.uint8).fill_(0x5A)
+        for w in p.ws:
+            w.fill_(rep)
+        p.reset()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(p.outs(), want)), rep
+        torch.randn(1000, 1000, device="cuda").sum().item()
+
+
+def test_two_streams_at_once(taw):
+    """Calls that overlap on two streams, each with its own workspace, do not meet."""
+    ps = [Pieces(2500, 512, 3001, 2), Pieces(700, 128, 40001, 3)]
+    want = []
+    for p in ps:
+        p.run(torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in p.outs()])
+        p.reset()
+    streams = [torch.cuda.Stream() for _ in ps]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for p, s in zip(ps, streams):
+            with torch.cuda.stream(s):
+                p.reset()
+            p.run(s)
+    torch.cuda.synchronize()
+    for p, w in zip(ps, want):
+        assert all(torch.equal(a, b) for a, b in zip(p.outs(), w))
+
+
+def test_offsets_past_32_bits(taw):
+    """A table, logits and a gradient of more than 2^31 elements: their last rows."""
+    V, H, T = 300_000, 8192, 700
+    G = torch.zeros((V, H), device="cuda")
+    ids = torch.full((T,), V - 1, dtype=torch.int64, device="cuda")
+    ids[::3] = V - 2
+    dx = torch.ones((T, H), dtype=torch.bfloat16, device="cuda")
+    d = taw.make_embed_desc(taw.TAW_BF16, T, H, V)
+    taw.taw_embed_bwd(d, ids, dx, G, scratch(taw.taw_embed_bwd_workspace_bytes(d)))
+    n = (T + 2) // 3
+    assert bool((G[V - 1] == T - n).all()) and bool((G[V - 2] == n).all()) and not G[:V - 2].any()
+    lst, st = taw.make_tensor_list([G.reshape(-1)]), taw.new_clip_state()
+    taw.taw_grad_norm(lst, 1.0, 1.0, st, scratch(taw.taw_grad_norm_workspace_bytes(lst)))
+    assert float(st.sumsq) == H * ((T - n) ** 2 + n ** 2)
+    taw.taw_grad_clip(lst, st)
+    assert torch.allclose(G[V - 1], (T - n) * st.coef.expand(H), rtol=1e-6)
+    del G
+    table = torch.zeros((V, H), dtype=torch.bfloat16, device="cuda")
+    table[V - 1], table[V - 2] = 3.0, 5.0
+    x = torch.empty((T, H), dtype=torch.bfloat16, device="cuda")
+    taw.taw_embed_fwd(d, ids, table, x)
+    assert bool((x[::3] == 5.0).all()) and bool((x[1::3] == 3.0).all())
+    del table, x
+    T, V = 40_000, 65_541
+    l = torch.empty((T, V), dtype=torch.bfloat16, device="cuda").normal_()
+    y = torch.randint(0, V, (T,), device="cuda", dtype=torch.int32)
+    d = taw.make_loss_desc(taw.TAW_BF16, T, V, flags=0)
+    loss, rows, lse, ws = torch.empty(2, device="cuda"), torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), scratch(taw.taw_loss_workspace_bytes(d))
+    tail = l[-3:].double().cpu().numpy()
+    taw.taw_loss_fwd_bwd(d, l, y, loss, rows, lse, l, ws)
+    r, e, _ = M.loss_fwd(tail, f64(y[-3:]).astype(np.int64))
+    assert np.allclose(f64(rows[-3:]), r, rtol=1e-5) and np.allclose(f64(lse[-3:]), e, rtol=1e-6)
+    g = M.loss_bwd(tail, f64(y[-3:]).astype(np.int64), e, np.ones(3))
+    assert np.all(np.abs(f64(l[-3:]) - g) <= (u8 + 1e-5) * np.abs(g) + 1e-9)
+
+
+def test_embed_bwd_very_many_tokens(taw):
+    T, H, V = 300_001, 8, 1000
+    rng = np.random.default_rng(4)
+    ids = zipf_ids(rng, T, V)
+    dx = on_gpu(rng.integers(-3, 4, (T, H)), torch.float32)          # whole numbers: every sum is exact
+    d = taw.make_embed_desc(taw.TAW_F32, T, H, V)
+    G = torch.empty((V, H), device="cuda")
+    taw.taw_embed_bwd(d, on_gpu(ids, torch.int64), dx, G, scratch(taw.taw_embed_bwd_workspace_bytes(d)))
+    assert np.array_equal(f64(G), M.embed_bwd(ids, f64(dx), V))
