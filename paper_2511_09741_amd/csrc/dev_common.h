@@ -70,6 +70,7 @@ template <> struct Vec<float, 2> {
   __device__ __forceinline__ void store_nt(float* p) const { __builtin_nontemporal_store(raw, reinterpret_cast<f32x2_t*>(p)); }
   __device__ __forceinline__ float get(int i) const { return raw[i]; }
   __device__ __forceinline__ void set(int i, float x) { raw[i] = x; }
+  __device__ __forceinline__ void pin() { asm volatile("" : "+v"(raw)); }
 };
 template <> struct Vec<bf16_t, 4> {
   bf16x4_t raw;
@@ -79,6 +80,7 @@ template <> struct Vec<bf16_t, 4> {
   __device__ __forceinline__ void store_nt(bf16_t* p) const { __builtin_nontemporal_store(raw, reinterpret_cast<bf16x4_t*>(p)); }
   __device__ __forceinline__ float get(int i) const { return (float)raw[i]; }
   __device__ __forceinline__ void set(int i, float x) { raw[i] = (bf16_t)x; }
+  __device__ __forceinline__ void pin() { asm volatile("" : "+v"(raw)); }
 };
 template <> struct Vec<bf16_t, 2> {
   bf16x2_t raw;
@@ -88,6 +90,7 @@ template <> struct Vec<bf16_t, 2> {
   __device__ __forceinline__ void store_nt(bf16_t* p) const { __builtin_nontemporal_store(raw, reinterpret_cast<bf16x2_t*>(p)); }
   __device__ __forceinline__ float get(int i) const { return (float)raw[i]; }
   __device__ __forceinline__ void set(int i, float x) { raw[i] = (bf16_t)x; }
+  __device__ __forceinline__ void pin() { asm volatile("" : "+v"(raw)); }
 };
 
 template <typename T> struct VecWidth;

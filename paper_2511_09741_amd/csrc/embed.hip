@@ -248,6 +248,8 @@ __global__ void __launch_bounds__(256) embed_rows_kernel(const int* __restrict__
       else r[k].load(dx + (int64_t)who[k] * ld_x + col);
     }
 #pragma unroll
+    for (int k = 0; k < U; ++k) r[k].pin();       // all are under way before the first is used
+#pragma unroll
     for (int k = 0; k < U; ++k) {
       if (q + k >= to) break;
       if (id[k] != cur) {
@@ -304,10 +306,11 @@ __global__ void __launch_bounds__(64 * kJoinWaves) embed_join_kernel(const int* 
   }
 }
 
-// A few tokens: one launch, no sort.  A workgroup per token and 64 VW columns lists the tokens with the same id; if its own is the first of them it
-// sums their rows, wavefront w the places w, w + 4, ... of the list, then the four in order.  The first zero_blocks workgroups zero the rows that no
-// token names.  Looking through the ids costs T * T / 64 loads for each column block, sorting them two launches more (few_tokens() has the line).
-constexpr int kFewTokens = 512, kZeroBlocks = 2048;
+// A few tokens: one launch, no sort.  A workgroup per token and 64 VW columns marks the tokens with the same id; if its own is the first of them it sums
+// their rows: of rows with fewer than 64 vectors a wavefront takes several at a time, in `groups` of lanes, and wavefront w the places w, w + 4, ... of
+// its groups in the list; then groups and wavefronts are added in order.  The first zero_blocks workgroups zero the rows that no token names.  Looking
+// through the ids costs T * T / 64 loads for each column block, sorting them two launches more (few_tokens() has the line).
+constexpr int kFewTokens = 2048, kZeroBlocks = 2048;
 template <typename T, int VW, typename TI>
 __global__ void __launch_bounds__(256) embed_few_kernel(const TI* __restrict__ ids, const T* __restrict__ dx, float* __restrict__ G, int T_, int H, int V, int64_t ld_table,
                                                         int64_t ld_x, float scale, int accumulate, int zero_blocks) {
@@ -334,42 +337,66 @@ __global__ void __launch_bounds__(256) embed_few_kernel(const TI* __restrict__ i
   __shared__ int list[kFewTokens];
   __shared__ fv_t red[4][64];
   const unsigned b = blockIdx.x - zero_blocks, ncb = (unsigned)((H + 64 * VW - 1) / (64 * VW));
-  const int t = (int)(b / ncb), col = (int)(b % ncb) * 64 * VW + lane * VW;
-  const int v = row_id(ids, t, V), nb = (T_ + 63) / 64;
+  const int t = (int)(b / ncb), v = row_id(ids, t, V), nb = (T_ + 63) / 64;
   if (v < 0) return;
-  for (int i = wave; i < nb; i += 4) {
-    const int at = i * 64 + lane;
-    const unsigned long long same = __ballot(at < T_ && row_id(ids, at < T_ ? at : 0, V) == v);
-    if (lane == 0) mask[i] = same;
+  int id[kFewTokens / 256];                     // all are under way before the first is looked at
+#pragma unroll
+  for (int k = 0; k < kFewTokens / 256; ++k) {
+    const int at = (k * 4 + wave) * 64 + lane;
+    id[k] = row_id(ids, at < T_ ? at : 0, V);
+  }
+#pragma unroll
+  for (int k = 0; k < kFewTokens / 256; ++k) {
+    const unsigned long long same = __ballot((k * 4 + wave) * 64 + lane < T_ && id[k] == v);
+    if (lane == 0) mask[k * 4 + wave] = same;
   }
   __syncthreads();
-  int n = 0;
-  for (int i = 0; i < nb; ++i) {
-    const unsigned long long same = mask[i];
-    if (i == (t >> 6) ? (same & ((1ull << (t & 63)) - 1)) != 0 : i < (t >> 6) && same) return;       // not the first
-    if ((i & 3) == wave && ((same >> lane) & 1)) list[n + __popcll(same & ((1ull << lane) - 1))] = i * 64 + lane;
-    n += __popcll(same);
+  // lane i looks at the 64 tokens i
+  const unsigned long long mine = lane < nb ? mask[lane] : 0;
+  const unsigned long long before = lane < (t >> 6) ? mine : lane == (t >> 6) ? mine & ((1ull << (t & 63)) - 1) : 0;
+  if (__ballot(before != 0)) return;            // not the first
+  int upto = __popcll(mine);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int up = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += up;
+  }
+  const int n = __shfl(upto, 63, 64);
+  if ((lane & 3) == wave) {
+    int at = upto - __popcll(mine);
+    for (unsigned long long left = mine; left; left &= left - 1) list[at++] = lane * 64 + __builtin_ctzll(left);
   }
   __syncthreads();
+  int width = 64;                               // lanes of a group
+  while (width > 1 && (width / 2) * VW >= H) width /= 2;
+  const int groups = 64 / width, col = (int)(b % ncb) * 64 * VW + (lane & (width - 1)) * VW;
   fv_t acc = fv_t(0.f);
   if (col < H) {
-    constexpr int U = 8;
-    for (int q = wave; q < n; q += 4 * U) {
+    const int step = 4 * groups;
+    int q = wave * groups + lane / width;
+    const auto rows = [&](auto u) {
+      constexpr int U = decltype(u)::value;
       Vec<T, VW> r[U];
 #pragma unroll
+      for (int k = 0; k < U; ++k) r[k].load(dx + (int64_t)list[q + k * step < n ? q + k * step : q] * ld_x + col);
+#pragma unroll
+      for (int k = 0; k < U; ++k) r[k].pin();     // all are under way before the first is used
+#pragma unroll
       for (int k = 0; k < U; ++k)
-        if (q + 4 * k < n) r[k].load(dx + (int64_t)list[q + 4 * k] * ld_x + col);
+        if (q + k * step < n)
 #pragma unroll
-      for (int k = 0; k < U; ++k) {
-        if (q + 4 * k >= n) break;
-#pragma unroll
-        for (int j = 0; j < VW; ++j) acc[j] += r[k].get(j);
-      }
-    }
+          for (int j = 0; j < VW; ++j) acc[j] += r[k].get(j);
+      q += U * step;
+    };
+    while (q + 8 * step < n) rows(std::integral_constant<int, 16>{});
+    while (q < n) rows(std::integral_constant<int, 4>{});      // most ids have one token or two
   }
+  for (int o = width; o < 64; o <<= 1)
+#pragma unroll
+    for (int j = 0; j < VW; ++j) acc[j] += __shfl_xor(acc[j], o, 64);
   red[wave][lane] = acc;
   __syncthreads();
-  if (wave || col >= H) return;
+  if (wave || lane >= width || col >= H) return;
   acc = scale * (((acc + red[1][lane]) + red[2][lane]) + red[3][lane]);
   fv_t* g = reinterpret_cast<fv_t*>(G + (int64_t)v * ld_table + col);
   *g = accumulate ? *g + acc : acc;
@@ -416,10 +443,11 @@ int launch_embed_fwd(const EmbedArgs& a, const void* ids, const void* table, voi
   });
 }
 
-// tokens of a piece: 64, or fewer where that leaves the chip fewer than 8 wavefronts a compute unit
+// Tokens of a piece: 64, or fewer where that leaves the chip fewer than 32 wavefronts a compute unit (8192 tokens of 4096 added to a shard: 75 us with 64,
+// 61 with 32, 58 with 16; 4503 of 1024: 24 us with 8, 27 with 16, 33 with 32; 32768 of 4096 the same with all).
 static int piece_of(int64_t T_, int64_t cpr) {
   int K = 64;
-  while (K > 8 && T_ * cpr < (int64_t)K * 131072) K /= 2;
+  while (K > 8 && T_ * cpr < (int64_t)K * 524288) K /= 2;
   return K;
 }
 
@@ -453,8 +481,8 @@ static int bwd_width_of(const EmbedArgs& a) {
   return w < 4 ? w : 4;
 }
 
-// Rows of 4096 added to a shard, us without and with the sort: 128 tokens 4.7 and 20, 512 17 and 20, 1024 47 and 24; rows of 1024, 1024 tokens 16 and 19,
-// but all of one id 29 and 14, which is why there is a limit of its own on the tokens.
+// Rows added to a shard of 32000, us without and with the sort, ids as text has them / a third of them one row: 512 tokens of 4096 12 / 17 and 20 / 17,
+// 1024 27 / 33 and 23 / 23; 1024 of 1024 8 / 16 and 19 / 19, 2048 17 / 29 and 22 / 21; 2048 of 256 9 / 18 and 19 / 19.
 static bool few_tokens(const EmbedArgs& a) { return a.T <= kFewTokens && (int64_t)a.T * a.T * ((a.H + 255) / 256) <= 1 << 22; }
 
 size_t embed_bwd_workspace_bytes(const EmbedArgs& a) { return few_tokens(a) ? 0 : embed_work(a, piece_of(a.T, a.H / bwd_width_of(a)), nullptr).bytes; }

@@ -40,7 +40,7 @@ def zipf_ids(rng, T, V):
 
 EMBED = [  # T, H, V
     (1, 1, 1), (1, 64, 509), (5, 7, 3), (63, 64, 5), (64, 8, 1000), (65, 100, 7), (128, 64, 509), (257, 520, 33), (333, 256, 32003),
-    (1000, 1, 2), (1024, 264, 70), (1025, 72, 64), (1100, 6, 300001), (1500, 1032, 300), (2049, 513, 20000), (4503, 1024, 32001), (9001, 20, 5), (20000, 8, 1)]
+    (1000, 1, 2), (1024, 264, 70), (2048, 24, 90), (2048, 256, 500), (1025, 72, 64), (1100, 6, 300001), (1500, 1032, 300), (2049, 513, 20000), (4503, 1024, 32001), (9001, 20, 5), (20000, 8, 1)]
 
 
 @pytest.mark.parametrize("T,H,V", EMBED)
