@@ -72,15 +72,15 @@ static SortShape sort_shape(int V) {
 // A workgroup goes through all the tokens to count its own ids by wavefront (each has a contiguous run of tokens) and the tokens of the workgroups
 // before it, which is where its part of the sorted sequence starts; then it places its own, which the wavefronts have listed in LDS (one that found
 // more than kSortList goes through its run again).  No workgroup waits for another, nothing is cleared beforehand.  The ids are read from L2 (256 times
-// 128 KiB at 32768 tokens).  Bound by latency, so it also zeroes the rows of G that no token names, whose stores nobody waits for.
+// 128 KiB at 32768 tokens).
 // perm: token at a sorted place; sid: its id; start[place_of(v)], start[own nb]: where the tokens of v start, and the number of tokens that name a row.
 constexpr int kSortList = 512;
 constexpr int kRunBits = 20;                   // T <= 2^24: a run has at most 2^20 tokens, and an id is one of 2^10 of its workgroup
 template <typename TI>
 __global__ void __launch_bounds__(1024) embed_sort_kernel(const TI* __restrict__ ids, int T_, int V, SortShape sh, int* __restrict__ perm, int* __restrict__ sid,
-                                                          int* __restrict__ start, float* __restrict__ G, int H, int64_t ld_table) {
+                                                          int* __restrict__ start) {
   extern __shared__ int cnt[];                 // [kSortWaves][own]
-  __shared__ int list[kSortWaves][kSortList], totals[kSortMaxOwn], wsum[kSortWaves], lsum[kSortWaves];
+  __shared__ int list[kSortWaves][kSortList], wsum[kSortWaves], lsum[kSortWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, R = sh.own, w0 = blockIdx.x;
   for (int i = threadIdx.x; i < kSortWaves * R; i += 1024) cnt[i] = 0;
   __syncthreads();
@@ -117,10 +117,8 @@ __global__ void __launch_bounds__(1024) embed_sort_kernel(const TI* __restrict__
   // where each id's tokens start, and within them each wavefront's
   int total = 0;
   const int r = threadIdx.x;                   // R <= 1024
-  if (r < R) {
+  if (r < R)
     for (int w = 0; w < kSortWaves; ++w) total += cnt[w * R + r];
-    totals[r] = total;
-  }
   int incl = total;
   for (int o = 1; o < 64; o <<= 1) {
     const int up = __shfl_up(incl, o, 64);
@@ -172,30 +170,28 @@ __global__ void __launch_bounds__(1024) embed_sort_kernel(const TI* __restrict__
       place(v >= 0 && sh.group_of(v) == w0, v >> sh.lb, t + lane);
     }
   }
-  if (!G) return;
-  const bool wide = ((H | ld_table) & 3) == 0;
-  for (int own = wave; own < R; own += kSortWaves) {
-    const int v = (own << sh.lb) | ((w0 - own) & ((1 << sh.lb) - 1));
-    if (totals[own] || v >= V) continue;
-    float* g = G + (int64_t)v * ld_table;
-    if (wide)
-      for (int c = 4 * lane; c < H; c += 256) __builtin_nontemporal_store(f32x4_t{0.f, 0.f, 0.f, 0.f}, reinterpret_cast<f32x4_t*>(g + c));
-    else
-      for (int c = lane; c < H; c += 64) g[c] = 0.f;
-  }
 }
 
 // Sums of pieces: a thread has one vector of columns of a piece.  part: [pieces][2][H]: the sum of the long id that a piece starts within (0), and of
-// the one that starts in it and goes on behind it (1).
+// the one that starts in it and goes on behind it (1).  The workgroups behind those of the pieces zero the rows that no token names, a vector a
+// thread (163 us for 32768 tokens of 4096; four rows a thread 173; zeroed by the sort's workgroups instead, beside its latency, 182).
 // Four columns a thread, also of bf16: the sums are stored 16 bytes a lane side by side (32768 tokens of 4096 into 32000 rows: 185 us with four, 192 with
 // eight).  STREAM: dx and G go past L2 (180 us; 4503 tokens of 1024, which L2 has room for: 24.8 against 23.3).
 template <typename T, int VW, bool STREAM>
 __global__ void __launch_bounds__(256) embed_rows_kernel(const int* __restrict__ perm, const int* __restrict__ sid, const int* __restrict__ start, const T* __restrict__ dx,
                                                          float* __restrict__ G, float* __restrict__ part, int H, SortShape sh, int64_t ld_table, int64_t ld_x,
-                                                         float scale, int accumulate, int K) {
+                                                         float scale, int accumulate, int K, unsigned piece_blocks, int V) {
   constexpr int U = 8;
   const unsigned cpr = (unsigned)(H / VW);
   typedef float fv_t __attribute__((ext_vector_type(VW), aligned(VW * 4 < 16 ? VW * 4 : 16)));
+  if (blockIdx.x >= piece_blocks) {
+    const uint64_t idx = (uint64_t)(blockIdx.x - piece_blocks) * 256 + threadIdx.x;
+    const int64_t v = (int64_t)(idx / cpr);
+    if (v >= V) return;
+    const int col = (int)(idx - v * cpr) * VW, at = sh.place_of((int)v);
+    if (start[at] == start[at + 1]) __builtin_nontemporal_store(fv_t(0.f), reinterpret_cast<fv_t*>(G + v * ld_table + col));
+    return;
+  }
   const uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   const uint64_t p = idx / cpr;
   const int col = (int)(idx - p * cpr) * VW;
@@ -505,15 +501,16 @@ int launch_embed_bwd(const EmbedArgs& a, const void* ids, const void* dx, float*
     const EmbedWork k = embed_work(a, K, ws);
     const SortShape sh = sort_shape(a.V);
     TAW_SET_LDS_LIMIT_ONCE((embed_sort_kernel<TI>), kSortWaves * kSortMaxOwn * sizeof(int));
-    hipLaunchKernelGGL((embed_sort_kernel<TI>), dim3(1u << sh.lb), dim3(1024), kSortWaves * sh.own * sizeof(int), st, (const TI*)ids, a.T, a.V, sh, k.perm, k.sid, k.start,
-                       a.accumulate ? nullptr : G, a.H, a.ld_table);
+    hipLaunchKernelGGL((embed_sort_kernel<TI>), dim3(1u << sh.lb), dim3(1024), kSortWaves * sh.own * sizeof(int), st, (const TI*)ids, a.T, a.V, sh, k.perm, k.sid, k.start);
     int e = last_err();
     if (e) return e;
     const uint64_t pieces = (a.T + K - 1) / K;
-    uint64_t blocks;
-    if (!grid_of(pieces * cpr, &blocks)) return (int)hipErrorInvalidValue;
+    uint64_t blocks, zero;
+    if (!grid_of(pieces * cpr, &blocks) || !grid_of(a.accumulate ? 0 : (uint64_t)a.V * cpr, &zero) || blocks + zero > 0x7fffffffu)
+      return (int)hipErrorInvalidValue;
     const auto rows = (uint64_t)a.T * a.H * sizeof(T) > kStreamBytes ? embed_rows_kernel<T, VW, true> : embed_rows_kernel<T, VW, false>;
-    hipLaunchKernelGGL(rows, dim3((unsigned)blocks), dim3(256), 0, st, k.perm, k.sid, k.start, (const T*)dx, G, k.part, a.H, sh, a.ld_table, a.ld_x, a.scale, a.accumulate, K);
+    hipLaunchKernelGGL(rows, dim3((unsigned)(blocks + zero)), dim3(256), 0, st, k.perm, k.sid, k.start, (const T*)dx, G, k.part, a.H, sh, a.ld_table, a.ld_x, a.scale, a.accumulate,
+                       K, (unsigned)blocks, a.V);
     e = last_err();
     if (e) return e;
     const unsigned cols = (unsigned)((a.H + 64 * VW - 1) / (64 * VW));
