@@ -7,8 +7,9 @@
  *
  * The general rules of taw.h hold: int status, device pointers unless a parameter says "host", nothing allocated, everything
  * enqueued on `stream` (the stream's device is the current one), no synchronisation, all validation on the host before the first
- * launch, device pointers 16-byte aligned (token ids and labels: aligned to their type).  Every result is deterministic: sums are
- * taken in an order that the sizes alone decide, and no floating-point atomics are used.
+ * launch, device pointers 16-byte aligned (token ids and labels: aligned to their type).  Every call can be captured into a graph.
+ * Calls, and captured graphs, that may run at the same time need workspaces (and clip states) of their own.  A call repeated gives
+ * the same bits: the order of every sum follows from the arguments, and there are no floating-point atomics.
  */
 #ifndef TAW_MODEL_H
 #define TAW_MODEL_H

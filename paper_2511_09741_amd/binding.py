@@ -314,6 +314,8 @@ def _index_type(ids, given) -> int:
         raise TawError(TAW_ERR_DTYPE, "TAW_ERR_DTYPE", f"token ids and labels are int32 or int64, not {ids.dtype}")
     if not ids.is_contiguous():
         raise TawError(TAW_ERR_SHAPE, "TAW_ERR_SHAPE", "token ids and labels must be contiguous")
+    if not ids.is_cuda:                     # what a data loader gives: the GPU would fault on it
+        raise TawError(TAW_ERR_UNSUPPORTED, "TAW_ERR_UNSUPPORTED", "token ids and labels must be in device memory")
     return kind
 
 
@@ -370,6 +372,8 @@ class TensorList:
                 raise TawError(TAW_ERR_DTYPE, "TAW_ERR_DTYPE", f"gradients are float32 or bfloat16, not {t.dtype}")
             if not t.is_contiguous():
                 raise TawError(TAW_ERR_SHAPE, "TAW_ERR_SHAPE", "gradients must be contiguous")
+            if not t.is_cuda:
+                raise TawError(TAW_ERR_UNSUPPORTED, "TAW_ERR_UNSUPPORTED", "gradients must be in device memory")
         self.array = (taw_tensor * max(1, len(self.tensors)))(*[taw_tensor(t.data_ptr(), t.numel(), kinds[t.dtype]) for t in self.tensors])
         self.count = len(self.tensors)
 

@@ -170,6 +170,7 @@ def test_embedding_refusals(lib):
     refuse(taw.TAW_ERR_NULL, taw.taw_embed_bwd, taw.make_embed_desc(taw.TAW_BF16, 0, 64, 100), None, None, None, None)     # but the shard is to be zeroed
     refuse(taw.TAW_ERR_DTYPE, taw.taw_embed_fwd, d, torch.zeros(8, dtype=torch.int16), OK, far)
     refuse(taw.TAW_ERR_SHAPE, taw.taw_embed_fwd, d, torch.zeros(16, dtype=torch.int64)[::2], OK, far)
+    refuse(taw.TAW_ERR_UNSUPPORTED, taw.taw_embed_fwd, d, torch.zeros(8, dtype=torch.int64), OK, far)      # in host memory
 
 
 @pytest.mark.parametrize("kw,code", [
@@ -244,7 +245,8 @@ def test_norm_and_clip_refusals(lib):
     n.count = -1
     refuse(taw.TAW_ERR_SHAPE, taw.taw_grad_clip, n, far)
     refuse(taw.TAW_ERR_DTYPE, taw.make_tensor_list, [torch.zeros(4, dtype=torch.float16)])
-    refuse(taw.TAW_ERR_SHAPE, taw.make_tensor_list, [torch.zeros(4, 4).t()])
+    refuse(taw.TAW_ERR_SHAPE, taw.make_tensor_list, [torch.zeros(4, 3).t()])
+    refuse(taw.TAW_ERR_UNSUPPORTED, taw.make_tensor_list, [torch.zeros(4)])
 
 
 def test_clipped_step_refusals(lib):
