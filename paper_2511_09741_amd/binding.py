@@ -297,25 +297,31 @@ def taw_last_error() -> str:
 def _nbytes(workspace, workspace_bytes):
     if workspace_bytes is not None:
         return workspace_bytes
-    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return 0 if workspace is None else workspace.nbytes
+
+
+def _refuse(status, name, detail):
+    raise TawError(status, name, detail)
+
+
+_index_types = {}       # torch dtype -> TAW_I32 / TAW_I64
 
 
 def _index_type(ids, given) -> int:
     """TAW_I32 or TAW_I64 of a tensor of token ids or labels, which has to be dense: read with another type it would be read past its end.
     An address has the type that the caller names."""
-    import torch
     if ids is None or isinstance(ids, int):
         return TAW_I64 if given is None else given
-    if ids.dtype == torch.int64:
-        kind = TAW_I64
-    elif ids.dtype == torch.int32:
-        kind = TAW_I32
-    else:
-        raise TawError(TAW_ERR_DTYPE, "TAW_ERR_DTYPE", f"token ids and labels are int32 or int64, not {ids.dtype}")
+    if not _index_types:
+        import torch
+        _index_types.update({torch.int32: TAW_I32, torch.int64: TAW_I64})
+    kind = _index_types.get(ids.dtype)
+    if kind is None:
+        _refuse(TAW_ERR_DTYPE, "TAW_ERR_DTYPE", f"token ids and labels are int32 or int64, not {ids.dtype}")
     if not ids.is_contiguous():
-        raise TawError(TAW_ERR_SHAPE, "TAW_ERR_SHAPE", "token ids and labels must be contiguous")
+        _refuse(TAW_ERR_SHAPE, "TAW_ERR_SHAPE", "token ids and labels must be contiguous")
     if not ids.is_cuda:                     # what a data loader gives: the GPU would fault on it
-        raise TawError(TAW_ERR_UNSUPPORTED, "TAW_ERR_UNSUPPORTED", "token ids and labels must be in device memory")
+        _refuse(TAW_ERR_UNSUPPORTED, "TAW_ERR_UNSUPPORTED", "token ids and labels must be in device memory")
     return kind
 
 

@@ -2,24 +2,28 @@
 //   sumsq = sum g^2 (fp64);  norm = |s| sqrt(sumsq);  coef = min(1, max_norm / norm)
 // Bound by memory: the norm reads every gradient once, the scaling in place reads and writes it once more.
 #include <cmath>
+#include <type_traits>
 
 #include "dev_common.h"
 #include "taw_internal.h"
 
 namespace taw {
 
-// Tensors travel as kernel arguments, so a call copies nothing to the device and can be captured; a longer list takes several launches.
-constexpr int kListMax = 120;
+// Tensors travel as kernel arguments, so a call copies nothing to the device and can be captured; a longer list takes several launches.  A short one
+// is a smaller argument (of 2.5 KB they made a launch from the host 1 us longer).
+template <int N>
 struct TensorList {
-  void* data[kListMax];
-  unsigned long long n[kListMax];
-  unsigned first[kListMax + 1];               // piece number of the tensor's first piece
-  unsigned char bf16[kListMax];
+  static constexpr int kMax = N;
+  void* data[N];
+  unsigned long long n[N];
+  unsigned first[N + 1];                      // piece number of the tensor's first piece
+  unsigned char bf16[N];
   int count;
   int piece;                                  // elements of a tensor that a workgroup takes at a time
 };
 
-__device__ __forceinline__ int tensor_of(const TensorList& l, unsigned piece) {
+template <typename L>
+__device__ __forceinline__ int tensor_of(const L& l, unsigned piece) {
   int lo = 0, hi = l.count - 1;               // the last tensor that starts at or before the piece
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -86,8 +90,8 @@ __device__ __forceinline__ double piece_sumsq(const T* __restrict__ p, int m) {
 }
 
 // f(data, elements) for the pieces of this workgroup; data points to float or bf16
-template <typename F>
-__device__ __forceinline__ void over_pieces(const TensorList& l, F f) {
+template <typename L, typename F>
+__device__ __forceinline__ void over_pieces(const L& l, F f) {
   const unsigned pieces = l.first[l.count];
   for (unsigned piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
     const int t = tensor_of(l, piece);
@@ -98,7 +102,8 @@ __device__ __forceinline__ void over_pieces(const TensorList& l, F f) {
   }
 }
 
-__global__ void __launch_bounds__(256) sumsq_kernel(const TensorList l, double* __restrict__ partials) {
+template <typename L>
+__global__ void __launch_bounds__(256) sumsq_kernel(const L l, double* __restrict__ partials) {
   double s = 0.0;
   over_pieces(l, [&](const auto* p, int m) { s += piece_sumsq(p, m); });
   s = block_sum_f64<4>(s);
@@ -159,7 +164,8 @@ __device__ __forceinline__ void piece_scale(T* __restrict__ p, int m, float c) {
   if (e < m) p[e] = (T)((float)p[e] * c);
 }
 
-__global__ void __launch_bounds__(256) clip_kernel(const TensorList l, const taw_clip_state* __restrict__ state) {
+template <typename L>
+__global__ void __launch_bounds__(256) clip_kernel(const L l, const taw_clip_state* __restrict__ state) {
   const float c = state->coef;
   if (c == 1.f || state->nonfinite) return;
   over_pieces(l, [&](auto* p, int m) { piece_scale(p, m, c); });
@@ -177,15 +183,15 @@ static int piece_of(const taw_tensor* t, int count) {
 }
 
 // cuts the list into launches; f(list, grid) returns a status
-template <typename F>
-static int over_list(const taw_tensor* t, int count, F f) {
-  TensorList l;
+template <typename L, typename F>
+static int over_list_as(const taw_tensor* t, int count, F f) {
+  L l;
   l.piece = piece_of(t, count);
   int i = 0;
   while (i < count) {
     l.count = 0;
     unsigned pieces = 0;
-    for (; i < count && l.count < kListMax; ++i) {
+    for (; i < count && l.count < L::kMax; ++i) {
       if (!t[i].n) continue;
       const unsigned long long np = (t[i].n + l.piece - 1) / l.piece;
       if (np > 0x7fffffffull) return (int)hipErrorInvalidValue;
@@ -204,17 +210,22 @@ static int over_list(const taw_tensor* t, int count, F f) {
   return 0;
 }
 
+template <typename F>
+static int over_list(const taw_tensor* t, int count, F f) {
+  return count <= 16 ? over_list_as<TensorList<16>>(t, count, f) : over_list_as<TensorList<120>>(t, count, f);
+}
+
 size_t grad_norm_workspace_bytes(const taw_tensor* t, int count) {
   size_t blocks = 0;
-  over_list(t, count, [&](const TensorList&, unsigned grid) { blocks += grid; return 0; });
+  over_list(t, count, [&](const auto&, unsigned grid) { blocks += grid; return 0; });
   return blocks * sizeof(double) + 16;
 }
 
 int launch_grad_sumsq(const taw_tensor* t, int count, int set, int finish, float max_norm, float grad_scale, taw_clip_state* state, void* ws, hipStream_t st) {
   double* partials = (double*)ws;
   int np = 0;
-  const int e = over_list(t, count, [&](const TensorList& l, unsigned grid) {
-    hipLaunchKernelGGL(sumsq_kernel, dim3(grid), dim3(256), 0, st, l, partials + np);
+  const int e = over_list(t, count, [&](const auto& l, unsigned grid) {
+    hipLaunchKernelGGL((sumsq_kernel<std::decay_t<decltype(l)>>), dim3(grid), dim3(256), 0, st, l, partials + np);
     np += (int)grid;
     return last_err();
   });
@@ -229,8 +240,8 @@ int launch_clip_coef(float max_norm, float grad_scale, taw_clip_state* state, hi
 }
 
 int launch_grad_clip(const taw_tensor* t, int count, const taw_clip_state* state, hipStream_t st) {
-  return over_list(t, count, [&](const TensorList& l, unsigned grid) {
-    hipLaunchKernelGGL(clip_kernel, dim3(grid), dim3(256), 0, st, l, state);
+  return over_list(t, count, [&](const auto& l, unsigned grid) {
+    hipLaunchKernelGGL((clip_kernel<std::decay_t<decltype(l)>>), dim3(grid), dim3(256), 0, st, l, state);
     return last_err();
   });
 }

@@ -230,6 +230,8 @@ __device__ __forceinline__ void empty_row(const TL* logits, TG* dlogits, int64_t
   for (int v = V + threadIdx.x; v < V_pad; v += NT) dlogits[t * ld_grad + v] = (TG)0.f;
 }
 
+constexpr int kEarlyRows = 1024;
+
 // =============================================================================== rows
 // A workgroup of NT threads per row, which stays packed in registers (MAXC vectors a thread) between its maximum, its sum of exponentials and its
 // gradient: the logits are read once.  MORE: of a row that is longer, the rest is summed on the way with a running maximum, and read a second time for the
@@ -242,16 +244,19 @@ __global__ void __launch_bounds__(NT) loss_row_kernel(const TL* logits, const La
   __shared__ float red[NW];
   const int64_t t = blockIdx.x;
   const int y = labels[t], tid = threadIdx.x;
+  const R row(logits, dlogits, t, V, ld, ld_grad);
+  typename R::vec_t x[MAXC];
+  const bool early = T_ <= kEarlyRows;             // few rows: the logits are not made to wait for the label, which may turn out to be none
+  if (early || y >= 0) {
+    if (row.count)
+#pragma unroll
+      for (int k = 0; k < MAXC; ++k) row.load(tid + k * NT < row.count ? tid + k * NT : row.count - 1, x[k]);      // always a load: none waits for a branch
+  }
   if (y < 0) {
     empty_row<NT, GRAD, SAME>(logits, dlogits, t, V, V_pad, ld, ld_grad, rows, lse_out);
     return;
   }
-  const R row(logits, dlogits, t, V, ld, ld_grad);
   const float ly = (float)logits[t * ld + y];      // before anything is written: dlogits may be the logits
-  typename R::vec_t x[MAXC];
-  if (row.count)
-#pragma unroll
-    for (int k = 0; k < MAXC; ++k) row.load(tid + k * NT < row.count ? tid + k * NT : row.count - 1, x[k]);      // always a load: none waits for a branch
   float counted = 1.f;
   if (GRAD && c.mean) {
     if (count) {
