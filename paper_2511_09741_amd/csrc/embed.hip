@@ -73,14 +73,15 @@ static SortShape sort_shape(int V) {
 // before it, which is where its part of the sorted sequence starts; then it places its own, which the wavefronts have listed in LDS (one that found
 // more than kSortList goes through its run again).  No workgroup waits for another, nothing is cleared beforehand.  The ids are read from L2 (256 times
 // 128 KiB at 32768 tokens).
-// perm: token at a sorted place; sid: its id; start[place_of(v)], start[own nb]: where the tokens of v start, and the number of tokens that name a row.
+// perm: token at a sorted place; sid: its id (0 and -1 behind the tokens that name a row); start[place_of(v)], start[own nb]: where the tokens of v start,
+// and how many name a row.
 constexpr int kSortList = 512;
 constexpr int kRunBits = 20;                   // T <= 2^24: a run has at most 2^20 tokens, and an id is one of 2^10 of its workgroup
 template <typename TI>
 __global__ void __launch_bounds__(1024) embed_sort_kernel(const TI* __restrict__ ids, int T_, int V, SortShape sh, int* __restrict__ perm, int* __restrict__ sid,
                                                           int* __restrict__ start) {
   extern __shared__ int cnt[];                 // [kSortWaves][own]
-  __shared__ int list[kSortWaves][kSortList], wsum[kSortWaves], lsum[kSortWaves];
+  __shared__ int list[kSortWaves][kSortList], wsum[kSortWaves], lsum[kSortWaves], placed;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, R = sh.own, w0 = blockIdx.x;
   for (int i = threadIdx.x; i < kSortWaves * R; i += 1024) cnt[i] = 0;
   __syncthreads();
@@ -139,9 +140,16 @@ __global__ void __launch_bounds__(1024) embed_sort_kernel(const TI* __restrict__
       cnt[w * R + r] = off;
       off += c;
     }
-    if (r == R - 1 && w0 == (int)gridDim.x - 1) start[w0 * R + R] = off;
+    if (r == R - 1) placed = off;
   }
   __syncthreads();
+  if (w0 == (int)gridDim.x - 1) {              // behind the last of all
+    if (threadIdx.x == 0) start[w0 * R + R] = placed;
+    for (int i = placed + threadIdx.x; i < T_; i += 1024) {
+      perm[i] = 0;
+      sid[i] = -1;
+    }
+  }
   // places 64 tokens of the run, in order: one turn for each different id among them
   auto place = [&](bool mine, int own, int token) {
     unsigned long long left = __ballot(mine);
@@ -180,7 +188,7 @@ __global__ void __launch_bounds__(1024) embed_sort_kernel(const TI* __restrict__
 template <typename T, int VW, bool STREAM>
 __global__ void __launch_bounds__(256) embed_rows_kernel(const int* __restrict__ perm, const int* __restrict__ sid, const int* __restrict__ start, const T* __restrict__ dx,
                                                          float* __restrict__ G, float* __restrict__ part, int H, SortShape sh, int64_t ld_table, int64_t ld_x,
-                                                         float scale, int accumulate, int K, unsigned piece_blocks, int V) {
+                                                         float scale, int accumulate, int K, unsigned piece_blocks, int V, int T_) {
   constexpr int U = 8;
   const unsigned cpr = (unsigned)(H / VW);
   typedef float fv_t __attribute__((ext_vector_type(VW), aligned(VW * 4 < 16 ? VW * 4 : 16)));
@@ -195,28 +203,51 @@ __global__ void __launch_bounds__(256) embed_rows_kernel(const int* __restrict__
   const uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   const uint64_t p = idx / cpr;
   const int col = (int)(idx - p * cpr) * VW;
-  const int n = start[sh.places() - 1];
-  if (p * K >= (uint64_t)n) return;
-  const int p0 = (int)p * K, p1 = p0 + K < n ? p0 + K : n;
+  const int p0 = (int)p * K;
+  if (p * K >= (uint64_t)T_) return;
+  int p1 = p0 + K < T_ ? p0 + K : T_;
+  int who[U], id[U];
+  Vec<T, VW> r[U];
+  // the first tokens are asked for before it is known which of them are this piece's, and so are their rows
+  const auto tokens = [&](int q, int to) {
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int at = q + k < to ? q + k : to - 1;
+      who[k] = perm[at];
+      id[k] = sid[at];
+    }
+  };
+  const auto load_rows = [&]() {
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (STREAM) r[k].load_nt(dx + (int64_t)who[k] * ld_x + col);
+      else r[k].load(dx + (int64_t)who[k] * ld_x + col);
+    }
+  };
+  tokens(p0, p1);
+  int last_id = sid[p1 - 1];
+  if (id[0] < 0) return;
+  if (last_id < 0) {                             // behind the last of all
+    p1 = start[sh.places() - 1];
+    last_id = sid[p1 - 1];
+  }
+  load_rows();
   int from = p0, to = p1;
   bool head = false, tail = false;
   {
-    const int v = sh.place_of(sid[p0]), s = start[v], e = start[v + 1];
+    const int v = sh.place_of(id[0]), w = sh.place_of(last_id), s = start[v], e = start[v + 1], s1 = start[w], e1 = start[w + 1];
     if (s < p0) {
       head = e - s > K;
-      if (!head) from = e;                     // its start's piece has it whole
+      if (!head) from = e;                       // its start's piece has it whole
     }
-  }
-  {
-    const int v = sh.place_of(sid[p1 - 1]), s = start[v], e = start[v + 1];
-    if (e > p1) {
-      tail = e - s > K;
-      if (!tail) to = e;
+    if (e1 > p1) {
+      tail = e1 - s1 > K;
+      if (!tail) to = e1;
     }
   }
   if (from >= to) return;
   fv_t acc = fv_t(0.f);
-  int cur = sid[from];
+  int cur = -1;
   auto flush = [&](bool last) {
     if (head || (last && tail)) {
       *reinterpret_cast<fv_t*>(part + ((int64_t)p * 2 + (head ? 0 : 1)) * H + col) = acc;
@@ -229,27 +260,19 @@ __global__ void __launch_bounds__(256) embed_rows_kernel(const int* __restrict__
     }
     head = false;
   };
-  for (int q = from; q < to; q += U) {
-    int who[U], id[U];
-    Vec<T, VW> r[U];
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-      const int at = q + k < to ? q + k : to - 1;
-      who[k] = perm[at];
-      id[k] = sid[at];
-    }
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-      if (STREAM) r[k].load_nt(dx + (int64_t)who[k] * ld_x + col);
-      else r[k].load(dx + (int64_t)who[k] * ld_x + col);
+  for (int q = p0; q < to; q += U) {
+    if (q != p0) {                               // U <= K: the first ones are there
+      tokens(q, to);
+      load_rows();
     }
 #pragma unroll
     for (int k = 0; k < U; ++k) r[k].pin();       // all are under way before the first is used
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       if (q + k >= to) break;
+      if (q + k < from) continue;
       if (id[k] != cur) {
-        flush(false);
+        if (cur >= 0) flush(false);
         cur = id[k];
         acc = fv_t(0.f);
       }
@@ -265,15 +288,14 @@ __global__ void __launch_bounds__(256) embed_rows_kernel(const int* __restrict__
 constexpr int kJoinWaves = 8, kJoinPieces = 16;
 template <int VW>
 __global__ void __launch_bounds__(64 * kJoinWaves) embed_join_kernel(const int* __restrict__ sid, const int* __restrict__ start, const float* __restrict__ part,
-                                                                     float* __restrict__ G, int H, SortShape sh, int64_t ld_table, float scale, int accumulate, int K) {
+                                                                     float* __restrict__ G, int H, SortShape sh, int64_t ld_table, float scale, int accumulate, int K, int T_) {
   typedef float fv_t __attribute__((ext_vector_type(VW)));
   __shared__ fv_t red[kJoinWaves][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = start[sh.places() - 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   // lane i looks at piece i: the id at its end, if that starts in it, goes on behind it and is long
   const int64_t end = ((int64_t)blockIdx.x * kJoinPieces + lane + 1) * K;
   int v = 0, np = 0;
-  if (lane < kJoinPieces && end < n) {
-    v = sid[end - 1];
+  if (lane < kJoinPieces && end < T_ && (v = sid[end - 1]) >= 0) {
     const int at = sh.place_of(v), s = start[at], e = start[at + 1];
     if (s >= end - K && e > end && e - s > K) np = (int)((e - 1) / K - (end / K - 1)) + 1;
   }
@@ -510,12 +532,12 @@ int launch_embed_bwd(const EmbedArgs& a, const void* ids, const void* dx, float*
       return (int)hipErrorInvalidValue;
     const auto rows = (uint64_t)a.T * a.H * sizeof(T) > kStreamBytes ? embed_rows_kernel<T, VW, true> : embed_rows_kernel<T, VW, false>;
     hipLaunchKernelGGL(rows, dim3((unsigned)(blocks + zero)), dim3(256), 0, st, k.perm, k.sid, k.start, (const T*)dx, G, k.part, a.H, sh, a.ld_table, a.ld_x, a.scale, a.accumulate,
-                       K, (unsigned)blocks, a.V);
+                       K, (unsigned)blocks, a.V, a.T);
     e = last_err();
     if (e) return e;
     const unsigned cols = (unsigned)((a.H + 64 * VW - 1) / (64 * VW));
     hipLaunchKernelGGL((embed_join_kernel<VW>), dim3((unsigned)((pieces + kJoinPieces - 1) / kJoinPieces), cols < 64 ? cols : 64), dim3(64 * kJoinWaves), 0, st, k.sid, k.start,
-                       k.part, G, a.H, sh, a.ld_table, a.scale, a.accumulate, K);
+                       k.part, G, a.H, sh, a.ld_table, a.scale, a.accumulate, K, a.T);
     return last_err();
   });
 }
