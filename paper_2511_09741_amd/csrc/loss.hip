@@ -26,6 +26,7 @@ struct Labels {
 template <int NW>
 __device__ __forceinline__ float block_sum(float x, float* red) {
   x = wave_sum(x);
+  if (NW == 1) return x;
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
   __syncthreads();
@@ -37,6 +38,7 @@ __device__ __forceinline__ float block_sum(float x, float* red) {
 template <int NW>
 __device__ __forceinline__ float block_max(float x, float* red) {
   x = wave_max(x);
+  if (NW == 1) return x;
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
   __syncthreads();
@@ -106,9 +108,8 @@ struct RowVecs {
       for (int j = 0; j < VW; ++j) out[(size_t)c * VW + j] = (TG)g[j];
     }
   }
-  // this thread's element of the edge, relative to the first vector; there is none where edge() is false
-  __device__ __forceinline__ bool edge(int* e) const {
-    const int i = threadIdx.x;
+  // the element of the edge that is thread i's, relative to the first vector; there is none where edge() is false
+  __device__ __forceinline__ bool edge(int i, int* e) const {
     *e = i < head ? i - head : i - head + count * VW;
     return i < head + tail;
   }
@@ -155,6 +156,7 @@ __device__ __forceinline__ void gradient(const R& row, unsigned c, const typenam
 // what a row comes to, from its maximum m, its sum of exponentials and (label smoothing) its sum of logits; the thread that is told to stores it
 struct RowResult {
   float scale, share, own;                         // gradient: scale * exp(l) - share, - own at the label
+  float loss = 0.f;                                // for the thread that stores it
   __device__ __forceinline__ RowResult(const Shift& sh, float m, float sum, float total, float ly, int V, const RowTerms& c, float counted, int64_t t, bool store,
                                        float* __restrict__ rows, float* __restrict__ lse_out) {
     const bool none = sum == 0.f;                  // nothing but -inf
@@ -163,7 +165,7 @@ struct RowResult {
       float r = none ? kInf : lse - (1.f - c.eps) * ly;
       if (c.eps != 0.f) r -= c.eps / (float)V * total;
       if (c.z != 0.f) r += c.z * lse * lse;
-      rows[t] = r;
+      rows[t] = loss = r;
       if (lse_out) lse_out[t] = lse;
     }
     const float up = none ? 0.f : c.mean ? c.grad_scale / counted : c.grad_scale;
@@ -200,8 +202,8 @@ struct Edge {
   int e;
   bool have;
   float l;
-  __device__ __forceinline__ Edge(const R& row, float eps, float& top, float& total) {
-    have = row.edge(&e);
+  __device__ __forceinline__ Edge(const R& row, int tid, float eps, float& top, float& total) {
+    have = row.edge(tid, &e);
     l = have ? (float)row.in[e] : -kInf;
     top = fmaxf(top, l);
     if (have && eps != 0.f) total += l;
@@ -214,20 +216,20 @@ struct Edge {
 
 // a row that is not counted
 template <int NT, bool GRAD, bool SAME, typename TL, typename TG>
-__device__ __forceinline__ void empty_row(const TL* logits, TG* dlogits, int64_t t, int V, int V_pad, int64_t ld, int64_t ld_grad, float* __restrict__ rows,
+__device__ __forceinline__ void empty_row(const TL* logits, TG* dlogits, int64_t t, int tid, int V, int V_pad, int64_t ld, int64_t ld_grad, float* __restrict__ rows,
                                           float* __restrict__ lse_out) {
   typedef RowVecs<TL, TG, SAME> R;
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
     rows[t] = 0.f;
     if (lse_out) lse_out[t] = 0.f;
   }
   if (!GRAD) return;
   const R row(logits, dlogits, t, V, ld, ld_grad);
   const float zero[R::VW] = {};
-  for (int i = threadIdx.x; i < row.count; i += NT) row.store(i, zero);
+  for (int i = tid; i < row.count; i += NT) row.store(i, zero);
   int e;
-  if (row.edge(&e)) row.out[e] = (TG)0.f;
-  for (int v = V + threadIdx.x; v < V_pad; v += NT) dlogits[t * ld_grad + v] = (TG)0.f;
+  if (row.edge(tid, &e)) row.out[e] = (TG)0.f;
+  for (int v = V + tid; v < V_pad; v += NT) dlogits[t * ld_grad + v] = (TG)0.f;
 }
 
 constexpr int kEarlyRows = 1024;
@@ -236,37 +238,26 @@ constexpr int kEarlyRows = 1024;
 // A workgroup of NT threads per row, which stays packed in registers (MAXC vectors a thread) between its maximum, its sum of exponentials and its
 // gradient: the logits are read once.  MORE: of a row that is longer, the rest is summed on the way with a running maximum, and read a second time for the
 // gradient, backwards (what was read last is the likeliest to be in a cache).
-template <typename TL, typename TG, int NT, int MAXC, bool MORE, bool GRAD, bool SAME>
-__global__ void __launch_bounds__(NT) loss_row_kernel(const TL* logits, const Labels labels, int T_, int V, int V_pad, int64_t ld, int64_t ld_grad, RowTerms c,
-                                                      const int* __restrict__ count, float* __restrict__ rows, float* __restrict__ lse_out, TG* dlogits) {
+// Row t by the threads tid = 0 .. NT - 1; counted: the rows that are, for the mean's gradient.  Returns the row's loss (tid 0).
+template <int NT, int MAXC, bool MORE, bool GRAD, bool SAME, typename TL, typename TG, typename C>
+__device__ __forceinline__ float loss_row(const TL* logits, const Labels& labels, int64_t t, int tid, bool early, int V, int V_pad, int64_t ld, int64_t ld_grad,
+                                          const RowTerms& c, C rows_counted, float* __restrict__ rows, float* __restrict__ lse_out, TG* dlogits, float* red) {
   typedef RowVecs<TL, TG, SAME> R;
   constexpr int NW = NT / 64;
-  __shared__ float red[NW];
-  const int64_t t = blockIdx.x;
-  const int y = labels[t], tid = threadIdx.x;
+  const int y = labels[t];
   const R row(logits, dlogits, t, V, ld, ld_grad);
   typename R::vec_t x[MAXC];
-  const bool early = T_ <= kEarlyRows;             // few rows: the logits are not made to wait for the label, which may turn out to be none
-  if (early || y >= 0) {
+  if (early || y >= 0) {                           // early: the logits are not made to wait for the label, which may turn out to be none
     if (row.count)
 #pragma unroll
       for (int k = 0; k < MAXC; ++k) row.load(tid + k * NT < row.count ? tid + k * NT : row.count - 1, x[k]);      // always a load: none waits for a branch
   }
   if (y < 0) {
-    empty_row<NT, GRAD, SAME>(logits, dlogits, t, V, V_pad, ld, ld_grad, rows, lse_out);
-    return;
+    empty_row<NT, GRAD, SAME>(logits, dlogits, t, tid, V, V_pad, ld, ld_grad, rows, lse_out);
+    return 0.f;
   }
   const float ly = (float)logits[t * ld + y];      // before anything is written: dlogits may be the logits
-  float counted = 1.f;
-  if (GRAD && c.mean) {
-    if (count) {
-      counted = (float)*count;
-    } else {
-      int n = 0;
-      for (int i = tid; i < T_; i += NT) n += labels[i] >= 0;
-      counted = block_sum<NW>((float)n, red);      // exact: T is small here
-    }
-  }
+  const float counted = GRAD && c.mean ? rows_counted() : 1.f;
   float top = -kInf, total = 0.f, sum = 0.f;
   const int n = row.count > tid ? (row.count - tid + NT - 1) / NT : 0;                 // vectors of this thread
   if (MORE) {
@@ -295,7 +286,7 @@ __global__ void __launch_bounds__(NT) loss_row_kernel(const TL* logits, const La
     }
   }
   const float before = top;                        // what sum is relative to
-  const Edge<R> edge(row, c.eps, top, total);
+  const Edge<R> edge(row, tid, c.eps, top, total);
   const auto exact_top = [&]() {
 #pragma unroll
     for (int k = 0; k < MAXC; ++k)
@@ -333,7 +324,7 @@ __global__ void __launch_bounds__(NT) loss_row_kernel(const TL* logits, const La
   }
   sum = block_sum<NW>(sum, red);
   const RowResult g(sh, m, sum, total, ly, V, c, counted, t, tid == 0, rows, lse_out);
-  if (!GRAD) return;
+  if (!GRAD) return g.loss;
 #pragma unroll
   for (int k = 0; k < MAXC; ++k) {
     x[k].pin();
@@ -352,6 +343,43 @@ __global__ void __launch_bounds__(NT) loss_row_kernel(const TL* logits, const La
   }
   edge.store(row, sh, g, y);
   for (int v = V + tid; v < V_pad; v += NT) dlogits[t * ld_grad + v] = (TG)0.f;
+  return g.loss;
+}
+
+template <typename TL, typename TG, int NT, int MAXC, bool MORE, bool GRAD, bool SAME>
+__global__ void __launch_bounds__(NT) loss_row_kernel(const TL* logits, const Labels labels, int T_, int V, int V_pad, int64_t ld, int64_t ld_grad, RowTerms c,
+                                                      const int* __restrict__ count, float* __restrict__ rows, float* __restrict__ lse_out, TG* dlogits) {
+  __shared__ float red[NT / 64];
+  const int tid = threadIdx.x;
+  const auto counted = [&]() {
+    if (count) return (float)*count;
+    int n = 0;
+    for (int i = tid; i < T_; i += NT) n += labels[i] >= 0;
+    return block_sum<NT / 64>((float)n, red);      // exact: T is small here
+  };
+  loss_row<NT, MAXC, MORE, GRAD, SAME>(logits, labels, blockIdx.x, tid, T_ <= kEarlyRows, V, V_pad, ld, ld_grad, c, counted, rows, lse_out, dlogits, red);
+}
+
+// Up to 16 short rows (kFewVecs vectors together): one workgroup for all of them and their sum, a wavefront on each, and so one launch.  8 rows of 1024 bf16:
+// 3.4 us, with gradient 4.1 (rows and sum in a launch each: 5.2, 6.3); 16 rows of 2048: 4.6, 6.5 (5.2, 6.4).  A second row a wavefront loses: 32 of 1024 take 6.1, 8.5 (5.1, 6.1).
+constexpr int kFewRows = 16, kFewVecs = 4096;
+template <typename TL, typename TG, bool GRAD, bool SAME>
+__global__ void __launch_bounds__(64 * kFewRows) loss_few_kernel(const TL* logits, const Labels labels, int T_, int V, int V_pad, int64_t ld, int64_t ld_grad, RowTerms c,
+                                                        float* __restrict__ loss, float* __restrict__ rows, float* __restrict__ lse_out, TG* dlogits) {
+  __shared__ double red[kFewRows];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int n = __popcll(__ballot(lane < T_ && labels[lane < T_ ? lane : 0] >= 0));
+  double s = 0.0;
+  if (wave < T_)
+    s = (double)loss_row<64, 8, false, GRAD, SAME>(logits, labels, wave, lane, true, V, V_pad, ld, ld_grad, c, [&]() { return (float)n; }, rows, lse_out, dlogits, nullptr);
+  if (lane == 0) red[wave] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.0;
+    for (int w = 0; w < kFewRows; ++w) s += red[w];
+    loss[0] = n == 0 ? 0.f : (float)(c.mean ? s / (double)n : s);
+    loss[1] = (float)n;
+  }
 }
 
 // The gradient from a saved lse: nothing is summed, so a row is cut into parts of kPart vectors.
@@ -393,7 +421,7 @@ __global__ void __launch_bounds__(256) loss_bwd_kernel(const TL* logits, const L
   }
   if (part) return;
   int e;
-  if (row.edge(&e)) row.out[e] = none ? 0.f : __builtin_fmaf(g.scale, sh.exp((float)row.in[e]), -g.share) - (e + row.head == y ? g.own : 0.f);
+  if (row.edge(threadIdx.x, &e)) row.out[e] = none ? 0.f : __builtin_fmaf(g.scale, sh.exp((float)row.in[e]), -g.share) - (e + row.head == y ? g.own : 0.f);
   for (int v = V + threadIdx.x; v < V_pad; v += 256) dlogits[t * ld_grad + v] = (TG)0.f;
 }
 
@@ -426,7 +454,7 @@ __global__ void __launch_bounds__(256) loss_part_kernel(const TL* __restrict__ l
     for (int k = 0; k < U; ++k) row.template load<true>(from + (k < n ? tid + k * NT : m_ - 1), x[k]);
   float top = -kInf, total = 0.f, sum = 0.f, edge = -kInf;
   int e;
-  if (part == 0 && row.edge(&e)) {
+  if (part == 0 && row.edge(tid, &e)) {
     top = edge = (float)row.in[e];
     total = edge;
   }
@@ -484,7 +512,7 @@ __global__ void __launch_bounds__(256) loss_part_grad_kernel(const TL* logits, c
   const R row(logits, dlogits, t, V, ld, ld_grad);
   const int from = part * len, left = row.count - from, m_ = left < len ? left : len, n = m_ > tid ? (m_ - tid + NT - 1) / NT : 0;
   int e;
-  const bool edge = part == 0 && row.edge(&e);
+  const bool edge = part == 0 && row.edge(tid, &e);
   if (y < 0) {
     const float zero[R::VW] = {};
     for (int k = 0; k < n; ++k) row.store(from + tid + k * NT, zero);
@@ -616,6 +644,11 @@ int launch_loss(const LossArgs& a, const void* logits, const void* labels, float
     constexpr int VW = 16 / sizeof(TL);
     const int vecs = a.V / VW, parts = parts_of(a, d != nullptr);
     PartSum* sums = (PartSum*)((char*)ws + 256 + rows_bytes(a.T));
+    if (a.T && a.T <= kFewRows && vecs <= 64 * 8 && a.T * vecs <= kFewVecs) {
+      const auto kernel = d ? loss_few_kernel<TL, TG, true, SAME> : loss_few_kernel<TL, TG, false, true>;
+      hipLaunchKernelGGL(kernel, dim3(1), dim3(64 * kFewRows), 0, st, l, y, a.T, a.V, a.V_pad, a.ld, a.ld_grad, c, loss, rows, lse, d);
+      return last_err();
+    }
     if (parts) {
       const int len = (vecs + parts - 1) / parts;
       hipLaunchKernelGGL((loss_part_kernel<TL>), dim3((unsigned)(a.T * parts)), dim3(256), 0, st, l, y, a.V, a.ld, a.eps, len, (unsigned)parts, sums);

@@ -236,6 +236,14 @@ def test_loss(taw, T, V, dtype, grad, ldt):
     check_loss(taw, T, V, dtype, grad, ldt, eps=0.1, z=1e-3, mean=False, scale=0.5, pad=(-V) % 64, odd=3)
 
 
+@pytest.mark.parametrize("T,V", [(9, 7), (16, 63), (17, 63), (16, 1025), (16, 2047), (16, 2056), (8, 4103), (8, 4104), (7, 2053)])
+@pytest.mark.parametrize("dtype,grad,ldt", TYPES)
+def test_loss_few_short_rows(taw, T, V, dtype, grad, ldt):
+    """On both sides of the sizes up to which one launch does it all."""
+    check_loss(taw, T, V, dtype, grad, ldt, eps=0.1, z=1e-3, pad=(-V) % 64, odd=5)
+    check_loss(taw, T, V, dtype, grad, ldt, mean=False, labels=np.full(T, V - 1))
+
+
 @pytest.mark.parametrize("T,V", [(5, 64), (6, 1003), (3, 32000), (3, 50001), (2, 131073)])
 @pytest.mark.parametrize("dtype,ldt", [("bf16", "i64"), ("f32", "i32")])
 def test_loss_in_place(taw, T, V, dtype, ldt):
