@@ -50,6 +50,7 @@ __device__ __forceinline__ float block_max(float x, float* red) {
 
 struct RowTerms {                 // of the loss
   float eps, z, grad_scale;
+  float each;                     // eps / V: the logits are weighted with it before they are summed, or classes masked by the type's lowest value overflow the sum
   int mean;
 };
 
@@ -153,24 +154,24 @@ __device__ __forceinline__ void gradient(const R& row, unsigned c, const typenam
   row.store(c, g);
 }
 
-// what a row comes to, from its maximum m, its sum of exponentials and (label smoothing) its sum of logits; the thread that is told to stores it
+// what a row comes to, from its maximum m, its sum of exponentials and (label smoothing) its weighted sum of logits; the thread that is told to stores it
 struct RowResult {
   float scale, share, own;                         // gradient: scale * exp(l) - share, - own at the label
   float loss = 0.f;                                // for the thread that stores it
-  __device__ __forceinline__ RowResult(const Shift& sh, float m, float sum, float total, float ly, int V, const RowTerms& c, float counted, int64_t t, bool store,
+  __device__ __forceinline__ RowResult(const Shift& sh, float m, float sum, float total, float ly, const RowTerms& c, float counted, int64_t t, bool store,
                                        float* __restrict__ rows, float* __restrict__ lse_out) {
     const bool none = sum == 0.f;                  // nothing but -inf
     const float lse = none ? -kInf : sh.lse(m, sum);
     if (store) {
       float r = none ? kInf : lse - (1.f - c.eps) * ly;
-      if (c.eps != 0.f) r -= c.eps / (float)V * total;
+      if (c.each != 0.f) r -= total;
       if (c.z != 0.f) r += c.z * lse * lse;
       rows[t] = loss = r;
       if (lse_out) lse_out[t] = lse;
     }
     const float up = none ? 0.f : c.mean ? c.grad_scale / counted : c.grad_scale;
     scale = none ? 0.f : up * (c.z != 0.f ? 1.f + 2.f * c.z * lse : 1.f) / sum;
-    share = up * c.eps / (float)V;
+    share = up * c.each;
     own = up * (1.f - c.eps);
   }
 };
@@ -202,11 +203,11 @@ struct Edge {
   int e;
   bool have;
   float l;
-  __device__ __forceinline__ Edge(const R& row, int tid, float eps, float& top, float& total) {
+  __device__ __forceinline__ Edge(const R& row, int tid, float each, float& top, float& total) {
     have = row.edge(tid, &e);
     l = have ? (float)row.in[e] : -kInf;
     top = fmaxf(top, l);
-    if (have && eps != 0.f) total += l;
+    if (have && each != 0.f) total = __builtin_fmaf(each, l, total);
   }
   template <typename G>
   __device__ __forceinline__ void store(const R& row, const Shift& sh, const G& g, int y) const {
@@ -281,12 +282,12 @@ __device__ __forceinline__ float loss_row(const TL* logits, const Labels& labels
           for (int j = 0; j < R::VW; ++j) {
             const float l = z[k].get(j);
             sum += __builtin_amdgcn_exp2f((l - ref) * kLog2e);
-            if (c.eps != 0.f) total += l;
+            if (c.each != 0.f) total = __builtin_fmaf(c.each, l, total);
           }
     }
   }
   const float before = top;                        // what sum is relative to
-  const Edge<R> edge(row, tid, c.eps, top, total);
+  const Edge<R> edge(row, tid, c.each, top, total);
   const auto exact_top = [&]() {
 #pragma unroll
     for (int k = 0; k < MAXC; ++k)
@@ -305,12 +306,12 @@ __device__ __forceinline__ float loss_row(const TL* logits, const Labels& labels
   } else {
     top = exact_top();
   }
-  if (c.eps != 0.f) {
+  if (c.each != 0.f) {
 #pragma unroll
     for (int k = 0; k < MAXC; ++k)
       if (k < n)
 #pragma unroll
-        for (int j = 0; j < R::VW; ++j) total += x[k].get(j);
+        for (int j = 0; j < R::VW; ++j) total = __builtin_fmaf(c.each, x[k].get(j), total);
     total = block_sum<NW>(total, red);
   }
   const float m = top == -kInf ? 0.f : top;
@@ -323,7 +324,7 @@ __device__ __forceinline__ float loss_row(const TL* logits, const Labels& labels
     if (k < n) sum_exp<R>(x[k], sh, sum);
   }
   sum = block_sum<NW>(sum, red);
-  const RowResult g(sh, m, sum, total, ly, V, c, counted, t, tid == 0, rows, lse_out);
+  const RowResult g(sh, m, sum, total, ly, c, counted, t, tid == 0, rows, lse_out);
   if (!GRAD) return g.loss;
 #pragma unroll
   for (int k = 0; k < MAXC; ++k) {
@@ -407,7 +408,7 @@ __global__ void __launch_bounds__(256) loss_bwd_kernel(const TL* logits, const L
   const float rest = sh.huge ? 1.f : __builtin_amdgcn_exp2f(-__builtin_fmaf(lse, sh.s, -sh.ms));     // what the rounding of lse s leaves out
   struct {
     float scale, share, own;
-  } const g{up * (c.z != 0.f ? 1.f + 2.f * c.z * lse : 1.f) * rest, up * c.eps / (float)V, up * (1.f - c.eps)};
+  } const g{up * (c.z != 0.f ? 1.f + 2.f * c.z * lse : 1.f) * rest, up * c.each, up * (1.f - c.eps)};
 #pragma unroll
   for (int k = 0; k < U; ++k) {
     const int i = first + k * 256;
@@ -438,7 +439,7 @@ struct PartSum {
 };
 
 template <typename TL>
-__global__ void __launch_bounds__(256) loss_part_kernel(const TL* __restrict__ logits, const Labels labels, int V, int64_t ld, float eps, int len, unsigned parts,
+__global__ void __launch_bounds__(256) loss_part_kernel(const TL* __restrict__ logits, const Labels labels, int V, int64_t ld, float each, int len, unsigned parts,
                                                         PartSum* __restrict__ out) {
   typedef RowVecs<TL, TL, true> R;
   constexpr int NT = 256, U = kSplitVecs / NT, NW = NT / 64;
@@ -456,7 +457,7 @@ __global__ void __launch_bounds__(256) loss_part_kernel(const TL* __restrict__ l
   int e;
   if (part == 0 && row.edge(tid, &e)) {
     top = edge = (float)row.in[e];
-    total = edge;
+    if (each != 0.f) total = each * edge;
   }
 #pragma unroll
   for (int k = 0; k < U; ++k)
@@ -473,11 +474,11 @@ __global__ void __launch_bounds__(256) loss_part_kernel(const TL* __restrict__ l
 #pragma unroll
       for (int j = 0; j < R::VW; ++j) {
         sum += sh.exp(x[k].get(j));
-        if (eps != 0.f) total += x[k].get(j);
+        if (each != 0.f) total = __builtin_fmaf(each, x[k].get(j), total);
       }
   }
   sum = block_sum<NW>(sum, red);
-  if (eps != 0.f) total = block_sum<NW>(total, red);
+  if (each != 0.f) total = block_sum<NW>(total, red);
   if (tid == 0) out[blockIdx.x] = PartSum{top, sum, total, part == 0 ? (float)logits[t * ld + y] : 0.f};
 }
 
@@ -536,7 +537,7 @@ __global__ void __launch_bounds__(256) loss_part_grad_kernel(const TL* logits, c
     }
     const float m = all.m == -kInf ? 0.f : all.m;
     const Shift sh(m);
-    const RowResult g(sh, m, all.sum, all.total, all.ly, V, c, counted, t, part == 0 && tid == 0, rows, lse_out);
+    const RowResult g(sh, m, all.sum, all.total, all.ly, c, counted, t, part == 0 && tid == 0, rows, lse_out);
 #pragma unroll
     for (int k = 0; k < U; ++k)
       if (k < n) gradient<false>(row, from + tid + k * NT, x[k], sh, g.scale, g.share, g.own, y);
@@ -548,7 +549,7 @@ __global__ void __launch_bounds__(256) loss_part_grad_kernel(const TL* logits, c
 
 // =============================================================================== sum of the rows' losses
 // parts != 0: the rows' losses are formed here, from the sums of their parts, a wavefront on each
-__global__ void __launch_bounds__(1024) loss_sum_kernel(float* rows, const Labels labels, int T_, int mean, float* __restrict__ loss, int parts, const PartSum* __restrict__ sums, int V,
+__global__ void __launch_bounds__(1024) loss_sum_kernel(float* rows, const Labels labels, int T_, int mean, float* __restrict__ loss, int parts, const PartSum* __restrict__ sums,
                                                         RowTerms c, float* __restrict__ lse_out) {
   __shared__ double red[16];
   __shared__ int redn[16];
@@ -564,7 +565,7 @@ __global__ void __launch_bounds__(1024) loss_sum_kernel(float* rows, const Label
       }
       const PartSum all = join_parts(sums + (size_t)t * parts, parts);
       const float m = all.m == -kInf ? 0.f : all.m;
-      const RowResult g(Shift(m), m, all.sum, all.total, all.ly, V, c, 1.f, t, first, rows, lse_out);
+      const RowResult g(Shift(m), m, all.sum, all.total, all.ly, c, 1.f, t, first, rows, lse_out);
     }
     __syncthreads();
   }
@@ -633,7 +634,7 @@ constexpr int kCountedInline = 1024;
 int launch_loss(const LossArgs& a, const void* logits, const void* labels, float* loss, float* rows, float* lse, void* dlogits, void* ws, hipStream_t st) {
   int* count = (int*)ws;
   if (!rows) rows = (float*)((char*)ws + 256);
-  const RowTerms c{a.eps, a.z, a.grad_scale, a.mean};
+  const RowTerms c{a.eps, a.z, a.grad_scale, a.eps / (float)a.V, a.mean};
   const Labels y{labels, a.label_type == IDX_I64, a.V};
   return by_types(a, [&](auto* pl, auto* pg, auto same) {
     using TL = std::remove_pointer_t<decltype(pl)>;
@@ -651,7 +652,7 @@ int launch_loss(const LossArgs& a, const void* logits, const void* labels, float
     }
     if (parts) {
       const int len = (vecs + parts - 1) / parts;
-      hipLaunchKernelGGL((loss_part_kernel<TL>), dim3((unsigned)(a.T * parts)), dim3(256), 0, st, l, y, a.V, a.ld, a.eps, len, (unsigned)parts, sums);
+      hipLaunchKernelGGL((loss_part_kernel<TL>), dim3((unsigned)(a.T * parts)), dim3(256), 0, st, l, y, a.V, a.ld, c.each, len, (unsigned)parts, sums);
       int e = last_err();
       if (e) return e;
       if (d) {
@@ -677,13 +678,13 @@ int launch_loss(const LossArgs& a, const void* logits, const void* labels, float
       const int e = last_err();
       if (e) return e;
     }
-    hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, st, rows, y, a.T, a.mean, loss, d ? 0 : parts, sums, a.V, c, lse);
+    hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, st, rows, y, a.T, a.mean, loss, d ? 0 : parts, sums, c, lse);
     return last_err();
   });
 }
 
 int launch_loss_bwd(const LossArgs& a, const void* logits, const void* labels, const float* lse, const float* dloss, void* dlogits, hipStream_t st) {
-  const RowTerms c{a.eps, a.z, 0.f, 0};
+  const RowTerms c{a.eps, a.z, 0.f, a.eps / (float)a.V, 0};
   const Labels y{labels, a.label_type == IDX_I64, a.V};
   return by_types(a, [&](auto* pl, auto* pg, auto same) {
     using TL = std::remove_pointer_t<decltype(pl)>;

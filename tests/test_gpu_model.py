@@ -282,6 +282,27 @@ def test_loss_masked_classes(taw, T, V, dtype, grad, ldt):
     check_loss(taw, T, V, dtype, grad, ldt, logits=l, labels=y, mean=False, odd=1)
 
 
+@pytest.mark.parametrize("T,V", [(8, 40), (20, 1001), (8, 32000), (8, 70001), (131, 70001)])
+@pytest.mark.parametrize("dtype,grad,ldt", TYPES)
+def test_loss_smoothing_over_masked_classes(taw, T, V, dtype, grad, ldt):
+    """Classes masked by the type's lowest value have a share of a smoothed label: the loss is large and finite, however many they are."""
+    rng = np.random.default_rng(V + 1)
+    l = rng.normal(0, 2, (T, V))
+    l[:, 5:] = np.where(rng.random((T, V - 5)) < 0.8, float(torch.finfo(DT[dtype][1]).min), l[:, 5:])
+    l[1] = float(torch.finfo(DT[dtype][1]).min)
+    y = rng.integers(0, 5, T)
+    _, out = check_loss(taw, T, V, dtype, grad, ldt, eps=0.1, logits=l, labels=y)
+    # the bounds of rows of such size say little about lse and the gradient, which are those of classes masked by -inf
+    l = f64(on_gpu(l, DT[dtype][1]))
+    l[l < -1e38] = -np.inf
+    rest = np.arange(T) != 1
+    l, y, e32, up = l[rest], y[rest], float(np.float32(0.1)), np.full(T - 1, 1.0 / T)
+    lse = M.loss_fwd(l, y)[1]
+    ref = M.loss_bwd(l, y, lse, up, e32)
+    bound = loss_bounds(l, lse, up, e32, 0.0, V, DT[grad][2])[2] + DT[grad][2] * np.abs(ref) + 2.0 ** -133
+    assert np.max(np.abs(f64(out)[rest] - ref) / bound) <= 1.0
+
+
 @pytest.mark.parametrize("T,V", [(6, 777), (6, 70001), (133, 70001)])
 @pytest.mark.parametrize("dtype,grad,ldt", TYPES)
 def test_loss_rows_of_infinities_and_nan(taw, dtype, grad, ldt, T, V):
