@@ -185,7 +185,7 @@ static int piece_of(const taw_tensor* t, int count, int most) {
   return n < ((size_t)1 << 22) ? 2048 : most;
 }
 constexpr int kSumPiece = 16384;
-constexpr unsigned kSumGrid = 2048, kScaleGrid = 0x7fffffff;
+constexpr unsigned kSumGrid = 2048, kScaleGrid = 1 << 23;
 
 // cuts the list into launches; f(list, grid) returns a status
 template <typename L, typename F>

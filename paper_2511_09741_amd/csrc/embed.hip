@@ -20,9 +20,9 @@ __device__ __forceinline__ int row_id(const TI* __restrict__ ids, int64_t t, int
 // frequent rows).  65536 tokens of 2048, 32000 rows: U = 1 94 us, 2 57 us, 4 58 us, 8 59 us; U = 4 with ordinary stores 80 us.
 template <typename T, int VW, int U, typename TI>
 __global__ void __launch_bounds__(256) embed_fwd_kernel(const TI* __restrict__ ids, const T* __restrict__ table, T* __restrict__ x, int T_, int H, int V, int64_t ld_table,
-                                                        int64_t ld_x, float scale) {
+                                                        int64_t ld_x, float scale, uint64_t block0) {
   const unsigned cpr = (unsigned)(H / VW);
-  const uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint64_t idx = (block0 + blockIdx.x) * 256 + threadIdx.x;
   const uint64_t group = idx / cpr;
   const int64_t t0 = (int64_t)group * U;
   if (t0 >= T_) return;
@@ -188,19 +188,20 @@ __global__ void __launch_bounds__(1024) embed_sort_kernel(const TI* __restrict__
 template <typename T, int VW, bool STREAM>
 __global__ void __launch_bounds__(256) embed_rows_kernel(const int* __restrict__ perm, const int* __restrict__ sid, const int* __restrict__ start, const T* __restrict__ dx,
                                                          float* __restrict__ G, float* __restrict__ part, int H, SortShape sh, int64_t ld_table, int64_t ld_x,
-                                                         float scale, int accumulate, int K, unsigned piece_blocks, int V, int T_) {
+                                                         float scale, int accumulate, int K, uint64_t piece_blocks, int V, int T_, uint64_t block0) {
   constexpr int U = 8;
   const unsigned cpr = (unsigned)(H / VW);
   typedef float fv_t __attribute__((ext_vector_type(VW), aligned(VW * 4 < 16 ? VW * 4 : 16)));
-  if (blockIdx.x >= piece_blocks) {
-    const uint64_t idx = (uint64_t)(blockIdx.x - piece_blocks) * 256 + threadIdx.x;
+  const uint64_t block = block0 + blockIdx.x;
+  if (block >= piece_blocks) {
+    const uint64_t idx = (block - piece_blocks) * 256 + threadIdx.x;
     const int64_t v = (int64_t)(idx / cpr);
     if (v >= V) return;
     const int col = (int)(idx - v * cpr) * VW, at = sh.place_of((int)v);
     if (start[at] == start[at + 1]) __builtin_nontemporal_store(fv_t(0.f), reinterpret_cast<fv_t*>(G + v * ld_table + col));
     return;
   }
-  const uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint64_t idx = block * 256 + threadIdx.x;
   const uint64_t p = idx / cpr;
   const int col = (int)(idx - p * cpr) * VW;
   const int p0 = (int)p * K;
@@ -443,20 +444,17 @@ static int by_types(const EmbedArgs& a, F f) {
   return a.id_type == IDX_I64 ? sized((float*)nullptr, (int64_t*)nullptr) : sized((float*)nullptr, (int32_t*)nullptr);
 }
 
-static bool grid_of(uint64_t threads, uint64_t* blocks) {
-  *blocks = (threads + 255) / 256;
-  return *blocks <= 0x7fffffffu;
-}
+static uint64_t blocks_of(uint64_t threads) { return (threads + 255) / 256; }
 
 int launch_embed_fwd(const EmbedArgs& a, const void* ids, const void* table, void* x, hipStream_t st) {
   return by_types(a, [&](auto* t, auto* i, auto w) {
     using T = std::remove_pointer_t<decltype(t)>;
     using TI = std::remove_pointer_t<decltype(i)>;
     constexpr int VW = decltype(w)::value, U = 2;
-    uint64_t blocks;
-    if (!grid_of((uint64_t)((a.T + U - 1) / U) * (a.H / VW), &blocks)) return (int)hipErrorInvalidValue;
-    hipLaunchKernelGGL((embed_fwd_kernel<T, VW, U, TI>), dim3((unsigned)blocks), dim3(256), 0, st, (const TI*)ids, (const T*)table, (T*)x, a.T, a.H, a.V, a.ld_table, a.ld_x,
-                       a.scale);
+    over_blocks(blocks_of((uint64_t)((a.T + U - 1) / U) * (a.H / VW)), kMostBlocks, [&](uint64_t block0, unsigned blocks) {
+      hipLaunchKernelGGL((embed_fwd_kernel<T, VW, U, TI>), dim3(blocks), dim3(256), 0, st, (const TI*)ids, (const T*)table, (T*)x, a.T, a.H, a.V, a.ld_table, a.ld_x, a.scale,
+                         block0);
+    });
     return last_err();
   });
 }
@@ -513,7 +511,7 @@ int launch_embed_bwd(const EmbedArgs& a, const void* ids, const void* dx, float*
     if (few_tokens(a)) {
       const int zero = a.accumulate ? 0 : a.V < kZeroBlocks ? a.V : kZeroBlocks;
       const uint64_t blocks = zero + (uint64_t)a.T * ((a.H + 64 * VW - 1) / (64 * VW));
-      if (blocks > 0x7fffffffu) return (int)hipErrorInvalidValue;
+      if (blocks > 1 << 23) return (int)hipErrorInvalidValue;      // there are fewer: few_tokens()
       hipLaunchKernelGGL((embed_few_kernel<T, VW, TI>), dim3((unsigned)blocks), dim3(256), 0, st, (const TI*)ids, (const T*)dx, G, a.T, a.H, a.V, a.ld_table, a.ld_x, a.scale,
                          a.accumulate, zero);
       return last_err();
@@ -522,17 +520,17 @@ int launch_embed_bwd(const EmbedArgs& a, const void* ids, const void* dx, float*
     const int K = piece_of(a.T, (int64_t)cpr);
     const EmbedWork k = embed_work(a, K, ws);
     const SortShape sh = sort_shape(a.V);
+    const uint64_t pieces = (a.T + K - 1) / K, blocks = blocks_of(pieces * cpr);
+    const uint64_t zero = blocks_of(a.accumulate ? 0 : (uint64_t)a.V * cpr);
     TAW_SET_LDS_LIMIT_ONCE((embed_sort_kernel<TI>), kSortWaves * kSortMaxOwn * sizeof(int));
     hipLaunchKernelGGL((embed_sort_kernel<TI>), dim3(1u << sh.lb), dim3(1024), kSortWaves * sh.own * sizeof(int), st, (const TI*)ids, a.T, a.V, sh, k.perm, k.sid, k.start);
     int e = last_err();
     if (e) return e;
-    const uint64_t pieces = (a.T + K - 1) / K;
-    uint64_t blocks, zero;
-    if (!grid_of(pieces * cpr, &blocks) || !grid_of(a.accumulate ? 0 : (uint64_t)a.V * cpr, &zero) || blocks + zero > 0x7fffffffu)
-      return (int)hipErrorInvalidValue;
     const auto rows = (uint64_t)a.T * a.H * sizeof(T) > kStreamBytes ? embed_rows_kernel<T, VW, true> : embed_rows_kernel<T, VW, false>;
-    hipLaunchKernelGGL(rows, dim3((unsigned)(blocks + zero)), dim3(256), 0, st, k.perm, k.sid, k.start, (const T*)dx, G, k.part, a.H, sh, a.ld_table, a.ld_x, a.scale, a.accumulate,
-                       K, (unsigned)blocks, a.V, a.T);
+    over_blocks(blocks + zero, kMostBlocks, [&](uint64_t block0, unsigned n) {
+      hipLaunchKernelGGL(rows, dim3(n), dim3(256), 0, st, k.perm, k.sid, k.start, (const T*)dx, G, k.part, a.H, sh, a.ld_table, a.ld_x, a.scale, a.accumulate, K, blocks, a.V, a.T,
+                         block0);
+    });
     e = last_err();
     if (e) return e;
     const unsigned cols = (unsigned)((a.H + 64 * VW - 1) / (64 * VW));

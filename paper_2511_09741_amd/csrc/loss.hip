@@ -16,6 +16,7 @@ constexpr float kInf = __builtin_huge_valf();
 struct Labels {
   const void* p;
   int wide, V;                // int64
+  Labels from(int64_t t) const { return Labels{static_cast<const char*>(p) + t * (wide ? 8 : 4), wide, V}; }
   __device__ __forceinline__ int operator[](int64_t t) const {
     const int64_t y = wide ? static_cast<const int64_t*>(p)[t] : static_cast<const int32_t*>(p)[t];
     return y >= 0 && y < V ? (int)y : -1;
@@ -55,18 +56,36 @@ struct RowTerms {                 // of the loss
 };
 
 // =============================================================================== counted rows
+__device__ __forceinline__ int wave_count(int n) {
+  for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+  return n;
+}
+
+// of each workgroup
 __global__ void __launch_bounds__(1024) loss_count_kernel(const Labels labels, int T_, int* __restrict__ count) {
   __shared__ int red[16];
   int n = 0;
-  for (int t = threadIdx.x; t < T_; t += 1024) n += labels[t] >= 0;
-  for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+  for (int t = blockIdx.x * 1024 + threadIdx.x; t < T_; t += gridDim.x * 1024) n += labels[t] >= 0;
+  n = wave_count(n);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
   __syncthreads();
   if (threadIdx.x == 0) {
     n = 0;
     for (int w = 0; w < 16; ++w) n += red[w];
-    *count = n;
+    count[blockIdx.x] = n;
   }
+}
+
+// of 64 workgroups
+__global__ void __launch_bounds__(64) loss_count_join_kernel(int* count) {
+  const int n = wave_count(count[threadIdx.x]);
+  if (threadIdx.x == 0) *count = n;
+}
+
+// by one thread
+__device__ __forceinline__ void store_loss(double s, int64_t n, int mean, float* __restrict__ loss) {
+  loss[0] = n == 0 ? 0.f : (float)(mean ? s / (double)n : s);
+  loss[1] = (float)n;
 }
 
 // =============================================================================== a row as vectors
@@ -378,8 +397,7 @@ __global__ void __launch_bounds__(64 * kFewRows) loss_few_kernel(const TL* logit
   if (threadIdx.x == 0) {
     s = 0.0;
     for (int w = 0; w < kFewRows; ++w) s += red[w];
-    loss[0] = n == 0 ? 0.f : (float)(c.mean ? s / (double)n : s);
-    loss[1] = (float)n;
+    store_loss(s, n, c.mean, loss);
   }
 }
 
@@ -548,9 +566,14 @@ __global__ void __launch_bounds__(256) loss_part_grad_kernel(const TL* logits, c
 }
 
 // =============================================================================== sum of the rows' losses
-// parts != 0: the rows' losses are formed here, from the sums of their parts, a wavefront on each
+struct LossSum {
+  double s;
+  int64_t n;
+};
+
+// parts != 0: the rows' losses are formed here, from the sums of their parts, a wavefront on each.  out: one workgroup of several, which leaves its sum
 __global__ void __launch_bounds__(1024) loss_sum_kernel(float* rows, const Labels labels, int T_, int mean, float* __restrict__ loss, int parts, const PartSum* __restrict__ sums,
-                                                        RowTerms c, float* __restrict__ lse_out) {
+                                                        RowTerms c, float* __restrict__ lse_out, LossSum* __restrict__ out) {
   __shared__ double red[16];
   __shared__ int redn[16];
   if (parts) {
@@ -571,14 +594,12 @@ __global__ void __launch_bounds__(1024) loss_sum_kernel(float* rows, const Label
   }
   double s = 0.0;
   int n = 0;
-  for (int t = threadIdx.x; t < T_; t += 1024) {
+  for (int t = blockIdx.x * 1024 + threadIdx.x; t < T_; t += gridDim.x * 1024) {
     s += (double)rows[t];
     n += labels[t] >= 0;
   }
-  for (int o = 32; o > 0; o >>= 1) {
-    s += __shfl_xor(s, o, 64);
-    n += __shfl_xor(n, o, 64);
-  }
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  n = wave_count(n);
   if ((threadIdx.x & 63) == 0) {
     red[threadIdx.x >> 6] = s;
     redn[threadIdx.x >> 6] = n;
@@ -591,9 +612,16 @@ __global__ void __launch_bounds__(1024) loss_sum_kernel(float* rows, const Label
       s += red[w];
       n += redn[w];
     }
-    loss[0] = n == 0 ? 0.f : (float)(mean ? s / (double)n : s);
-    loss[1] = (float)n;
+    if (out) out[blockIdx.x] = LossSum{s, n};
+    else store_loss(s, n, mean, loss);
   }
+}
+
+__global__ void __launch_bounds__(64) loss_sum_join_kernel(const LossSum* __restrict__ sums, int mean, float* __restrict__ loss) {
+  double s = sums[threadIdx.x].s;
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  const int n = wave_count((int)sums[threadIdx.x].n);
+  if (threadIdx.x == 0) store_loss(s, n, mean, loss);
 }
 
 // =============================================================================== launchers
@@ -610,10 +638,11 @@ static int parts_of(const LossArgs& a, bool grad) {
   return least > kSplitMax ? 0 : parts < kSplitMax ? (int)parts : kSplitMax;
 }
 
-// the count; the rows' losses where the caller has no use for them; the sums of parts
+// 64 counts; 64 sums; the rows' losses where the caller has no use for them; the sums of parts
+constexpr size_t kHeadBytes = 64 * sizeof(int) + 64 * sizeof(LossSum);
 static size_t rows_bytes(int T_) { return ((size_t)T_ * 4 + 255) / 256 * 256; }
 size_t loss_workspace_bytes(const LossArgs& a) {
-  return 256 + rows_bytes(a.T) + (size_t)a.T * parts_of(a, true) * sizeof(PartSum);
+  return kHeadBytes + rows_bytes(a.T) + (size_t)a.T * parts_of(a, true) * sizeof(PartSum);
 }
 
 template <typename F>
@@ -630,10 +659,12 @@ static int by_types(const LossArgs& a, F f) {
 // Rows up to which a workgroup counts the labels itself.  us so and with a launch for the count: 256 rows of 1000 7.8 and 10.3, 1024 rows of 1000 10.2 and
 // 10.4, of 32000 26.9 and 29.6; 2048 rows of 1000 13.6 and 10.3, 3000 rows of 32000 81 and 76.
 constexpr int kCountedInline = 1024;
+// Rows up to which one workgroup counts the labels, and one adds up the losses, not 64 and another launch.
+constexpr int kOneGroup = 16384;
 
 int launch_loss(const LossArgs& a, const void* logits, const void* labels, float* loss, float* rows, float* lse, void* dlogits, void* ws, hipStream_t st) {
   int* count = (int*)ws;
-  if (!rows) rows = (float*)((char*)ws + 256);
+  if (!rows) rows = (float*)((char*)ws + kHeadBytes);
   const RowTerms c{a.eps, a.z, a.grad_scale, a.eps / (float)a.V, a.mean};
   const Labels y{labels, a.label_type == IDX_I64, a.V};
   return by_types(a, [&](auto* pl, auto* pg, auto same) {
@@ -643,8 +674,9 @@ int launch_loss(const LossArgs& a, const void* logits, const void* labels, float
     const TL* l = (const TL*)logits;
     TG* d = (TG*)dlogits;
     constexpr int VW = 16 / sizeof(TL);
+    const bool many = a.T > kOneGroup;
     const int vecs = a.V / VW, parts = parts_of(a, d != nullptr);
-    PartSum* sums = (PartSum*)((char*)ws + 256 + rows_bytes(a.T));
+    PartSum* sums = (PartSum*)((char*)ws + kHeadBytes + rows_bytes(a.T));
     if (a.T && a.T <= kFewRows && vecs <= 64 * 8 && a.T * vecs <= kFewVecs) {
       const auto kernel = d ? loss_few_kernel<TL, TG, true, SAME> : loss_few_kernel<TL, TG, false, true>;
       hipLaunchKernelGGL(kernel, dim3(1), dim3(64 * kFewRows), 0, st, l, y, a.T, a.V, a.V_pad, a.ld, a.ld_grad, c, loss, rows, lse, d);
@@ -662,12 +694,19 @@ int launch_loss(const LossArgs& a, const void* logits, const void* labels, float
         if (e) return e;
       }
     } else if (a.T) {
-      if (d && a.mean && a.T > kCountedInline) hipLaunchKernelGGL(loss_count_kernel, dim3(1), dim3(1024), 0, st, y, a.T, count);
-      else count = nullptr;
+      if (d && a.mean && a.T > kCountedInline) {
+        hipLaunchKernelGGL(loss_count_kernel, dim3(many ? 64 : 1), dim3(1024), 0, st, y, a.T, count);
+        if (many) hipLaunchKernelGGL(loss_count_join_kernel, dim3(1), dim3(64), 0, st, count);
+      } else {
+        count = nullptr;
+      }
 #define TAW_LOSS(NT, MAXC, MORE)                                                                                                                    \
   do {                                                                                                                                              \
     const auto kernel = d ? loss_row_kernel<TL, TG, NT, MAXC, MORE, true, SAME> : loss_row_kernel<TL, TG, NT, MAXC, MORE, false, true>;             \
-    hipLaunchKernelGGL(kernel, dim3((unsigned)a.T), dim3(NT), 0, st, l, y, a.T, a.V, a.V_pad, a.ld, a.ld_grad, c, count, rows, lse, d);             \
+    over_blocks(a.T, kMostBlocks, [&](int64_t t, unsigned rows_) {                                                                                  \
+      hipLaunchKernelGGL(kernel, dim3(rows_), dim3(NT), 0, st, l + t * a.ld, y.from(t), a.T, a.V, a.V_pad, a.ld, a.ld_grad, c, count, rows + t,     \
+                         lse ? lse + t : lse, d ? d + t * a.ld_grad : d);                                                                           \
+    });                                                                                                                                             \
   } while (0)
       if (vecs <= 64 * 8) TAW_LOSS(64, 8, false);
       else if (vecs <= 256 * 8) TAW_LOSS(256, 8, false);
@@ -678,7 +717,9 @@ int launch_loss(const LossArgs& a, const void* logits, const void* labels, float
       const int e = last_err();
       if (e) return e;
     }
-    hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, st, rows, y, a.T, a.mean, loss, d ? 0 : parts, sums, c, lse);
+    LossSum* part = (LossSum*)((char*)ws + 64 * sizeof(int));
+    hipLaunchKernelGGL(loss_sum_kernel, dim3(many ? 64 : 1), dim3(1024), 0, st, rows, y, a.T, a.mean, loss, d ? 0 : parts, sums, c, lse, many ? part : nullptr);
+    if (many) hipLaunchKernelGGL(loss_sum_join_kernel, dim3(1), dim3(64), 0, st, part, a.mean, loss);
     return last_err();
   });
 }
@@ -690,10 +731,11 @@ int launch_loss_bwd(const LossArgs& a, const void* logits, const void* labels, c
     using TL = std::remove_pointer_t<decltype(pl)>;
     using TG = std::remove_pointer_t<decltype(pg)>;
     constexpr int VW = 16 / sizeof(TL);
-    const uint64_t parts = a.V < VW ? 1 : (a.V / VW + kPart - 1) / kPart, blocks = parts * a.T;
-    if (blocks > 0x7fffffffu) return (int)hipErrorInvalidValue;
-    hipLaunchKernelGGL((loss_bwd_kernel<TL, TG, decltype(same)::value>), dim3((unsigned)blocks), dim3(256), 0, st, (const TL*)logits, y, a.V, a.V_pad, a.ld, a.ld_grad, c, lse, dloss,
-                       (TG*)dlogits, (unsigned)parts);
+    const unsigned parts = a.V < VW ? 1u : (unsigned)((a.V / VW + kPart - 1) / kPart);
+    over_blocks(a.T, kMostBlocks / parts & ~7ull, [&](int64_t t, unsigned rows) {      // multiples of 8 rows: as aligned as the first
+      hipLaunchKernelGGL((loss_bwd_kernel<TL, TG, decltype(same)::value>), dim3(rows * parts), dim3(256), 0, st, (const TL*)logits + t * a.ld, y.from(t), a.V, a.V_pad, a.ld,
+                         a.ld_grad, c, lse + t, dloss + t, (TG*)dlogits + t * a.ld_grad, parts);
+    });
     return last_err();
   });
 }

@@ -194,6 +194,12 @@ int launch_attn_bwd_mfma(int B, int S, int nh, const void* qkv, const void* o, c
                          float* scratch, void* dqkv, const float* rope_table, int form, hipStream_t st);
 
 // ---- what stands around the layers (embed.hip, loss.hip, clip.hip) ------------------------------
+// A launch has fewer than 2^32 threads: more than kMostBlocks workgroups (of at most 512) are several launches, f(first, number).
+constexpr uint64_t kMostBlocks = 1 << 22;
+template <typename F>
+inline void over_blocks(uint64_t blocks, uint64_t most, F f) {
+  for (uint64_t b = 0; b < blocks; b += most) f(b, (unsigned)(blocks - b < most ? blocks - b : most));
+}
 enum { IDX_I32 = 0, IDX_I64 = 1 };
 struct EmbedArgs {
   int dtype, id_type, T, H, V;

@@ -341,6 +341,13 @@ def test_loss_with_nothing_counted(taw, T):
     assert f64(loss).tolist() == [0.0, 0.0]
 
 
+@pytest.mark.parametrize("T,V", [(1500, 9), (16384, 17), (16385, 17), (70001, 33)])
+def test_loss_rows_of_several_workgroups(taw, T, V):
+    """Labels counted, and losses added up, by one workgroup and by several."""
+    check_loss(taw, T, V, "bf16", "bf16", "i64", eps=0.1)
+    check_loss(taw, T, V, "f32", "f32", "i32", mean=False)
+
+
 @pytest.mark.parametrize("T,V", [(2500, 70), (5000, 33)])
 def test_loss_many_rows(taw, T, V):
     check_loss(taw, T, V, "bf16", "bf16", "i32")
@@ -676,3 +683,45 @@ def test_embed_bwd_very_many_tokens(taw):
     G = torch.empty((V, H), device="cuda")
     taw.taw_embed_bwd(d, on_gpu(ids, torch.int64), dx, G, scratch(taw.taw_embed_bwd_workspace_bytes(d)))
     assert np.array_equal(f64(G), M.embed_bwd(ids, f64(dx), V))
+
+
+def test_loss_of_the_most_rows(taw):
+    """2^24 rows: more threads than one dimension of a launch has."""
+    T, V = 1 << 24, 8
+    l, y = torch.randn((T, V), device="cuda").bfloat16(), torch.randint(-1, V, (T,), device="cuda", dtype=torch.int32)
+    d = taw.make_loss_desc(taw.TAW_BF16, T, V, grad_scale=float(T))
+    loss, rows, lse, out = torch.zeros(2, device="cuda"), torch.zeros(T, device="cuda"), torch.zeros(T, device="cuda"), torch.empty_like(l)
+    taw.taw_loss_fwd_bwd(d, l, y, loss, rows, lse, out, scratch(taw.taw_loss_workspace_bytes(d)))
+    live, L = y >= 0, l.double()
+    n = int(live.sum())
+    ref = torch.logsumexp(L, 1)
+    want = torch.where(live, ref - L.gather(1, y.clamp(min=0).long()[:, None])[:, 0], 0.0)
+    # values below 8: 2^-20 is over ten roundings of them
+    assert float((rows - want).abs().max()) < 2 ** -20 and float((lse - torch.where(live, ref, 0.0)).abs().max()) < 2 ** -20
+    assert float(loss[1]) == n and abs(float(loss[0]) - float(want.sum()) / n) < 2 ** -20
+    g = (torch.exp(L - ref[:, None]) - torch.nn.functional.one_hot(y.clamp(min=0).long(), V)) * live[:, None] * (T / n)
+    near = g.abs() * u8 + 2.0 ** -18
+    assert bool(((out.double() - g).abs() <= near).all())
+    out.fill_(9.0)
+    taw.taw_loss_bwd(d, l, y, lse, torch.full((T,), T / n, device="cuda"), out)
+    assert bool(((out.double() - g).abs() <= near).all())
+
+
+def test_embed_of_the_most_threads(taw):
+    """Rows of odd length, a thread an element: more threads than one dimension of a launch has."""
+    T, H, V = (1 << 20) + 3, 8193, 7
+    table, ids = torch.randn((V, H), device="cuda").bfloat16(), torch.randint(0, V, (T,), device="cuda")
+    x = torch.empty((T, H), dtype=torch.bfloat16, device="cuda")
+    taw.taw_embed_fwd(taw.make_embed_desc(taw.TAW_BF16, T, H, V), ids, table, x)
+    for t in range(0, T, 1 << 16):
+        assert torch.equal(x[t:t + (1 << 16)], table[ids[t:t + (1 << 16)]])
+    del x
+    T, H, V = 3000, 4097, (1 << 20) + 5
+    ids, dx = torch.randint(0, V, (T,), device="cuda"), torch.ones((T, H), dtype=torch.bfloat16, device="cuda")
+    ids[:100] = V - 1
+    d = taw.make_embed_desc(taw.TAW_BF16, T, H, V)
+    G = torch.full((V, H), float("nan"), device="cuda")
+    taw.taw_embed_bwd(d, ids, dx, G, scratch(taw.taw_embed_bwd_workspace_bytes(d)))
+    count = torch.bincount(ids, minlength=V).float()
+    for v in range(0, V, 1 << 16):
+        assert bool((G[v:v + (1 << 16)] == count[v:v + (1 << 16), None]).all())
