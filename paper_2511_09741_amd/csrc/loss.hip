@@ -366,18 +366,21 @@ __device__ __forceinline__ float loss_row(const TL* logits, const Labels& labels
   return g.loss;
 }
 
-template <typename TL, typename TG, int NT, int MAXC, bool MORE, bool GRAD, bool SAME>
-__global__ void __launch_bounds__(NT) loss_row_kernel(const TL* logits, const Labels labels, int T_, int V, int V_pad, int64_t ld, int64_t ld_grad, RowTerms c,
-                                                      const int* __restrict__ count, float* __restrict__ rows, float* __restrict__ lse_out, TG* dlogits) {
+// ROWS: of a workgroup, more than one where a wavefront takes a row (NT = 64)
+template <typename TL, typename TG, int ROWS, int NT, int MAXC, bool MORE, bool GRAD, bool SAME>
+__global__ void __launch_bounds__(NT* ROWS) loss_row_kernel(const TL* logits, const Labels labels, int T_, int V, int V_pad, int64_t ld, int64_t ld_grad, RowTerms c,
+                                                            const int* __restrict__ count, float* __restrict__ rows, float* __restrict__ lse_out, TG* dlogits, int n_rows) {
+  static_assert(ROWS == 1 || NT == 64, "");
   __shared__ float red[NT / 64];
-  const int tid = threadIdx.x;
+  const int tid = ROWS == 1 ? threadIdx.x : threadIdx.x & 63, t = ROWS == 1 ? blockIdx.x : blockIdx.x * ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (ROWS > 1 && t >= n_rows) return;
   const auto counted = [&]() {
     if (count) return (float)*count;
     int n = 0;
     for (int i = tid; i < T_; i += NT) n += labels[i] >= 0;
     return block_sum<NT / 64>((float)n, red);      // exact: T is small here
   };
-  loss_row<NT, MAXC, MORE, GRAD, SAME>(logits, labels, blockIdx.x, tid, T_ <= kEarlyRows, V, V_pad, ld, ld_grad, c, counted, rows, lse_out, dlogits, red);
+  loss_row<NT, MAXC, MORE, GRAD, SAME>(logits, labels, t, tid, T_ <= kEarlyRows, V, V_pad, ld, ld_grad, c, counted, rows, lse_out, dlogits, red);
 }
 
 // Up to 16 short rows (kFewVecs vectors together): one workgroup for all of them and their sum, a wavefront on each, and so one launch.  8 rows of 1024 bf16:
@@ -401,25 +404,28 @@ __global__ void __launch_bounds__(64 * kFewRows) loss_few_kernel(const TL* logit
   }
 }
 
-// The gradient from a saved lse: nothing is summed, so a row is cut into parts of kPart vectors.
+// The gradient from a saved lse: nothing is summed, so a row is cut into parts of kPart vectors, and ROWS short ones share a workgroup (65536 rows of 256 bf16
+// 12 us, 44 with a workgroup each).
 constexpr int kPart = 1024;
-template <typename TL, typename TG, bool SAME>
+template <typename TL, typename TG, bool SAME, int ROWS>
 __global__ void __launch_bounds__(256) loss_bwd_kernel(const TL* logits, const Labels labels, int V, int V_pad, int64_t ld, int64_t ld_grad, RowTerms c,
-                                                       const float* __restrict__ lse_in, const float* __restrict__ dloss, TG* dlogits, unsigned parts) {
+                                                       const float* __restrict__ lse_in, const float* __restrict__ dloss, TG* dlogits, unsigned parts, unsigned n_rows) {
   typedef RowVecs<TL, TG, SAME> R;
-  constexpr int U = kPart / 256;
-  const int64_t t = blockIdx.x / parts;
-  const unsigned part = blockIdx.x - (unsigned)t * parts;
+  constexpr int U = kPart / 256, NT = 256 / ROWS;
+  const int tid = threadIdx.x % NT;
+  const int64_t t = ROWS == 1 ? blockIdx.x / parts : blockIdx.x * ROWS + threadIdx.x / NT;
+  if (ROWS > 1 && t >= n_rows) return;
+  const unsigned part = ROWS == 1 ? blockIdx.x - (unsigned)t * parts : 0;
   const int y = labels[t];
   const R row(logits, dlogits, t, V, ld, ld_grad);
   const float lse = lse_in[t];
   const bool none = y < 0 || lse == -kInf;
-  const int first = part * kPart + threadIdx.x;
+  const int first = part * kPart + tid;
   typename R::vec_t x[U];
   if (!none) {
 #pragma unroll
     for (int k = 0; k < U; ++k)
-      if (first + k * 256 < row.count) row.load(first + k * 256, x[k]);
+      if (first + k * NT < row.count) row.load(first + k * NT, x[k]);
   }
   const Shift sh(lse);
   const float up = none ? 0.f : dloss[t];
@@ -429,7 +435,7 @@ __global__ void __launch_bounds__(256) loss_bwd_kernel(const TL* logits, const L
   } const g{up * (c.z != 0.f ? 1.f + 2.f * c.z * lse : 1.f) * rest, up * c.each, up * (1.f - c.eps)};
 #pragma unroll
   for (int k = 0; k < U; ++k) {
-    const int i = first + k * 256;
+    const int i = first + k * NT;
     if (i >= row.count) break;
     if (none) {
       const float zero[R::VW] = {};
@@ -440,8 +446,8 @@ __global__ void __launch_bounds__(256) loss_bwd_kernel(const TL* logits, const L
   }
   if (part) return;
   int e;
-  if (row.edge(threadIdx.x, &e)) row.out[e] = none ? 0.f : __builtin_fmaf(g.scale, sh.exp((float)row.in[e]), -g.share) - (e + row.head == y ? g.own : 0.f);
-  for (int v = V + threadIdx.x; v < V_pad; v += 256) dlogits[t * ld_grad + v] = (TG)0.f;
+  if (row.edge(tid, &e)) row.out[e] = none ? 0.f : __builtin_fmaf(g.scale, sh.exp((float)row.in[e]), -g.share) - (e + row.head == y ? g.own : 0.f);
+  for (int v = V + tid; v < V_pad; v += NT) dlogits[t * ld_grad + v] = (TG)0.f;
 }
 
 // =============================================================================== few rows
@@ -660,6 +666,9 @@ static int by_types(const LossArgs& a, F f) {
 // 10.4, of 32000 26.9 and 29.6; 2048 rows of 1000 13.6 and 10.3, 3000 rows of 32000 81 and 76.
 constexpr int kCountedInline = 1024;
 // Rows up to which one workgroup counts the labels, and one adds up the losses, not 64 and another launch.
+// More rows than this that a wavefront holds lie four to a workgroup: with gradient, 65536 rows of 4000 bf16 187 us (201 with a workgroup to a row), 16384 57 and 60,
+// 4096 the same.  Those of at most a vector a lane always do, with registers for no more: 2^20 rows of 256 453 us (516 with room for eight), 333 of 30 the same.
+constexpr int kWaveRows = 2047;
 constexpr int kOneGroup = 16384;
 
 int launch_loss(const LossArgs& a, const void* logits, const void* labels, float* loss, float* rows, float* lse, void* dlogits, void* ws, hipStream_t st) {
@@ -700,19 +709,21 @@ int launch_loss(const LossArgs& a, const void* logits, const void* labels, float
       } else {
         count = nullptr;
       }
-#define TAW_LOSS(NT, MAXC, MORE)                                                                                                                    \
-  do {                                                                                                                                              \
-    const auto kernel = d ? loss_row_kernel<TL, TG, NT, MAXC, MORE, true, SAME> : loss_row_kernel<TL, TG, NT, MAXC, MORE, false, true>;             \
-    over_blocks(a.T, kMostBlocks, [&](int64_t t, unsigned rows_) {                                                                                  \
-      hipLaunchKernelGGL(kernel, dim3(rows_), dim3(NT), 0, st, l + t * a.ld, y.from(t), a.T, a.V, a.V_pad, a.ld, a.ld_grad, c, count, rows + t,     \
-                         lse ? lse + t : lse, d ? d + t * a.ld_grad : d);                                                                           \
-    });                                                                                                                                             \
+#define TAW_LOSS(ROWS, NT, MAXC, MORE)                                                                                                                         \
+  do {                                                                                                                                                         \
+    const auto kernel = d ? loss_row_kernel<TL, TG, ROWS, NT, MAXC, MORE, true, SAME> : loss_row_kernel<TL, TG, ROWS, NT, MAXC, MORE, false, true>;            \
+    over_blocks(a.T, kMostBlocks, [&](int64_t t, unsigned n) {                                                                                                 \
+      hipLaunchKernelGGL(kernel, dim3((n + ROWS - 1) / ROWS), dim3(NT * ROWS), 0, st, l + t * a.ld, y.from(t), a.T, a.V, a.V_pad, a.ld, a.ld_grad, c, count,   \
+                         rows + t, lse ? lse + t : lse, d ? d + t * a.ld_grad : d, (int)n);                                                                    \
+    });                                                                                                                                                        \
   } while (0)
-      if (vecs <= 64 * 8) TAW_LOSS(64, 8, false);
-      else if (vecs <= 256 * 8) TAW_LOSS(256, 8, false);
-      else if (vecs <= 512 * 8) TAW_LOSS(512, 8, false);
-      else if (vecs <= kHeldVecs) TAW_LOSS(512, 16, false);
-      else TAW_LOSS(512, 16, true);
+      if (vecs <= 64) TAW_LOSS(4, 64, 1, false);
+      else if (vecs <= 64 * 8 && a.T > kWaveRows) TAW_LOSS(4, 64, 8, false);
+      else if (vecs <= 64 * 8) TAW_LOSS(1, 64, 8, false);
+      else if (vecs <= 256 * 8) TAW_LOSS(1, 256, 8, false);
+      else if (vecs <= 512 * 8) TAW_LOSS(1, 512, 8, false);
+      else if (vecs <= kHeldVecs) TAW_LOSS(1, 512, 16, false);
+      else TAW_LOSS(1, 512, 16, true);
 #undef TAW_LOSS
       const int e = last_err();
       if (e) return e;
@@ -731,11 +742,16 @@ int launch_loss_bwd(const LossArgs& a, const void* logits, const void* labels, c
     using TL = std::remove_pointer_t<decltype(pl)>;
     using TG = std::remove_pointer_t<decltype(pg)>;
     constexpr int VW = 16 / sizeof(TL);
-    const unsigned parts = a.V < VW ? 1u : (unsigned)((a.V / VW + kPart - 1) / kPart);
-    over_blocks(a.T, kMostBlocks / parts & ~7ull, [&](int64_t t, unsigned rows) {      // multiples of 8 rows: as aligned as the first
-      hipLaunchKernelGGL((loss_bwd_kernel<TL, TG, decltype(same)::value>), dim3(rows * parts), dim3(256), 0, st, (const TL*)logits + t * a.ld, y.from(t), a.V, a.V_pad, a.ld,
-                         a.ld_grad, c, lse + t, dloss + t, (TG*)dlogits + t * a.ld_grad, parts);
-    });
+    const unsigned vecs = a.V / VW, parts = vecs ? (vecs + kPart - 1) / kPart : 1;
+#define TAW_LOSS_BWD(ROWS)                                                                                                                                             \
+  over_blocks(a.T, kMostBlocks / parts & ~7ull, [&](int64_t t, unsigned n) { /* multiples of 8 rows: as aligned as the first */                                        \
+    hipLaunchKernelGGL((loss_bwd_kernel<TL, TG, decltype(same)::value, ROWS>), dim3((n + ROWS - 1) / ROWS * parts), dim3(256), 0, st, (const TL*)logits + t * a.ld,    \
+                       y.from(t), a.V, a.V_pad, a.ld, a.ld_grad, c, lse + t, dloss + t, (TG*)dlogits + t * a.ld_grad, parts, n);                                       \
+  })
+    if (vecs <= kPart / 16) TAW_LOSS_BWD(16);
+    else if (vecs <= kPart / 4) TAW_LOSS_BWD(4);
+    else TAW_LOSS_BWD(1);
+#undef TAW_LOSS_BWD
     return last_err();
   });
 }
