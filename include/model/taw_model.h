@@ -54,8 +54,10 @@ int taw_embed_bwd(const taw_embed_desc* desc, const void* ids, int32_t id_type, 
  *   dl_v = up ((1 + 2 z lse) exp(l_v - lse) - (1 - eps) [v = y] - eps/V)
  * with up = grad_scale, divided by the number of counted rows with TAW_LOSS_MEAN (taw_loss_fwd_bwd), or dloss_rows[t] (taw_loss_bwd).
  * A row whose label is outside [0, V) (-100 and its like) is not counted: its logits are not looked at, its loss, lse and gradient
- * are 0.  Logits of -inf are masked classes: probability and gradient 0 (as a label: loss +inf).  A counted row with nothing but
- * -inf has lse -inf, loss +inf and a gradient of 0; +inf or NaN in a counted row make all of its results NaN.
+ * are 0.  Logits of -inf are masked classes of probability 0, which leaves them the rest of the formulas: the loss is +inf where
+ * such a class is the label or has a share eps/V of it, and its gradient -up times what it has of the label (0 without smoothing).
+ * (The type's lowest value is a finite logit like any other.)  A counted row with nothing but -inf has lse -inf, loss +inf and a gradient of 0;
+ * +inf or NaN in a counted row make all of its results NaN.
  * Everything is computed in fp32 (sums over rows in fp64) from the logits as stored, and dlogits is rounded once.
  * dlogits [T, V_pad] of grad_dtype with row stride ld_grad: columns V .. V_pad-1 (a vocabulary padded for the products around
  * this call) are written as zeros; columns of logits beyond V are not read.  dlogits may be logits itself where types and strides

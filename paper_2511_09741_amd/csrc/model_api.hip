@@ -18,6 +18,19 @@ static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 // bytes from the first element of a [rows, cols] matrix with row stride ld to behind its last one
 static size_t span(int64_t rows, int64_t cols, int64_t ld, size_t e) { return rows > 0 ? (size_t)((rows - 1) * ld + cols) * e : 0; }
 
+struct Piece {
+  const void* p;
+  size_t n;
+};
+// whether one of the first `written` pieces shares memory with another piece (NULL shares none)
+template <size_t N>
+static bool any_overlap(const Piece (&x)[N], size_t written) {
+  for (size_t i = 0; i < written; ++i)
+    for (size_t k = i + 1; k < N; ++k)
+      if (x[i].p && x[k].p && overlap(x[i].p, x[i].n, x[k].p, x[k].n)) return true;
+  return false;
+}
+
 static bool bad_dtype(int32_t d) { return d != TAW_F32 && d != TAW_BF16; }
 
 static int check_ids(const void* ids, int32_t id_type, const char* what) {
@@ -105,9 +118,12 @@ static int check_loss(const taw_loss_desc* d, LossArgs* a) {
   return TAW_OK;
 }
 
+static size_t logits_bytes(const LossArgs& a) { return span(a.T, a.V, a.ld, dt_size(a.dtype)); }
+static size_t dlogits_bytes(const LossArgs& a) { return span(a.T, a.V_pad, a.ld_grad, dt_size(a.grad_dtype)); }
+static size_t label_bytes(const LossArgs& a) { return (size_t)a.T * (a.label_type == TAW_I64 ? 8 : 4); }
+
 static int check_dlogits(const LossArgs& a, const void* logits, const void* dlogits) {
-  const size_t nl = span(a.T, a.V, a.ld, dt_size(a.dtype)), ng = span(a.T, a.V_pad, a.ld_grad, dt_size(a.grad_dtype));
-  if (overlap(logits, nl, dlogits, ng) && !(logits == dlogits && a.dtype == a.grad_dtype && a.ld == a.ld_grad))
+  if (overlap(logits, logits_bytes(a), dlogits, dlogits_bytes(a)) && !(logits == dlogits && a.dtype == a.grad_dtype && a.ld == a.ld_grad))
     return fail(TAW_ERR_SHAPE, "dlogits overlaps the logits and is not the logits, with their type and row stride");
   return TAW_OK;
 }
@@ -135,7 +151,10 @@ static int loss_call(const taw_loss_desc* desc, const void* logits, const void* 
   }
   TAW_REQUIRE_PTR(loss); TAW_REQUIRE_PTR(workspace);
   TAW_REQUIRE_ALIGNED(loss); TAW_REQUIRE_ALIGNED(workspace); TAW_REQUIRE_ALIGNED(loss_rows); TAW_REQUIRE_ALIGNED(lse);
-  if (workspace_bytes < loss_workspace_bytes(a)) return fail(TAW_ERR_WORKSPACE, "workspace_bytes=%zu < required %zu", workspace_bytes, loss_workspace_bytes(a));
+  const size_t need = loss_workspace_bytes(a), rows = (size_t)a.T * 4;
+  if (workspace_bytes < need) return fail(TAW_ERR_WORKSPACE, "workspace_bytes=%zu < required %zu", workspace_bytes, need);
+  const Piece all[] = {{loss, 8}, {loss_rows, rows}, {lse, rows}, {workspace, need}, {labels, label_bytes(a)}, {logits, logits_bytes(a)}, {dlogits, grad ? dlogits_bytes(a) : 0}};
+  if (any_overlap(all, 5)) return fail(TAW_ERR_SHAPE, "buffers of the loss overlap");
   TAW_LAUNCH(launch_loss(a, logits, labels, loss, loss_rows, lse, grad ? dlogits : nullptr, workspace, (hipStream_t)stream), "loss");
   return TAW_OK;
 }
@@ -163,6 +182,8 @@ extern "C" int taw_loss_bwd(const taw_loss_desc* desc, const void* logits, const
   TAW_REQUIRE_ALIGNED(logits); TAW_REQUIRE_ALIGNED(lse); TAW_REQUIRE_ALIGNED(dloss_rows); TAW_REQUIRE_ALIGNED(dlogits);
   rc = check_dlogits(a, logits, dlogits);
   if (rc) return rc;
+  const Piece all[] = {{dlogits, dlogits_bytes(a)}, {labels, label_bytes(a)}, {lse, (size_t)a.T * 4}, {dloss_rows, (size_t)a.T * 4}};
+  if (any_overlap(all, 1)) return fail(TAW_ERR_SHAPE, "dlogits overlaps the labels or what is known of the rows");
   TAW_LAUNCH(launch_loss_bwd(a, logits, labels, lse, dloss_rows, dlogits, (hipStream_t)stream), "loss backward");
   return TAW_OK;
 }
@@ -197,6 +218,12 @@ static int sumsq_call(const taw_tensor* tensors, int32_t count, int set, int fin
   TAW_REQUIRE_PTR(state); TAW_REQUIRE_PTR(workspace); TAW_REQUIRE_ALIGNED(state); TAW_REQUIRE_ALIGNED(workspace);
   const size_t need = grad_norm_workspace_bytes(tensors, count);
   if (workspace_bytes < need) return fail(TAW_ERR_WORKSPACE, "workspace_bytes=%zu < required %zu", workspace_bytes, need);
+  if (overlap(state, sizeof(*state), workspace, need)) return fail(TAW_ERR_SHAPE, "the state overlaps the workspace");
+  for (int32_t i = 0; i < count; ++i) {
+    const size_t n = tensors[i].n * dt_size(tensors[i].dtype);
+    if (overlap(tensors[i].data, n, state, sizeof(*state)) || overlap(tensors[i].data, n, workspace, need))
+      return fail(TAW_ERR_SHAPE, "tensor %d overlaps the state or the workspace", i);
+  }
   TAW_LAUNCH(launch_grad_sumsq(tensors, count, set, finish, max_norm, grad_scale, state, workspace, (hipStream_t)stream), "gradient norm");
   return TAW_OK;
 }

@@ -206,6 +206,14 @@ def test_loss_refusals(lib):
     same = taw.make_loss_desc(taw.TAW_F32, 8, 100, ld=128)
     refuse(taw.TAW_ERR_SHAPE, taw.taw_loss_bwd, same, L, Y, R, E, L)                       # ... and one row stride
     refuse(taw.TAW_ERR_SHAPE, taw.taw_loss_bwd, taw.make_loss_desc(taw.TAW_F32, 8, 100), L, Y, R, E, L + 16)
+    for i, k in ((2, 0), (2, 1), (2, 3), (3, 0), (3, 4), (3, 5), (4, 1), (4, 5), (6, 0), (6, 1), (6, 2), (6, 3), (6, 5), (1, 5)):
+        a = list(good)
+        a[i] = a[k]                                                                        # two of the buffers are one
+        refuse(taw.TAW_ERR_SHAPE, taw.taw_loss_fwd_bwd, d, *a)
+    for i in (1, 2, 3):
+        a = [L, Y, R, E, D]
+        a[i] = D
+        refuse(taw.TAW_ERR_SHAPE, taw.taw_loss_bwd, d, *a)
     for i in range(5):
         a = [L, Y, R, E, D]
         a[i] = None
@@ -235,6 +243,9 @@ def test_norm_and_clip_refusals(lib):
     refuse(taw.TAW_ERR_ALIGN, taw.taw_grad_sumsq, lst((OK + 8, 4, 0)), 0, far, far + 4096, ws)
     refuse(taw.TAW_ERR_DTYPE, taw.taw_grad_sumsq, lst((OK, 4, 2)), 0, far, far + 4096, ws)
     refuse(taw.TAW_ERR_SHAPE, taw.taw_grad_sumsq, lst((OK, 2**48 + 1, 0)), 0, far, far + 4096, 1 << 40)
+    refuse(taw.TAW_ERR_SHAPE, taw.taw_grad_norm, ok, 1.0, 1.0, far, far + 16, 1 << 20)                # the workspace over the state
+    refuse(taw.TAW_ERR_SHAPE, taw.taw_grad_norm, ok, 1.0, 1.0, OK + 240, far, ws)
+    refuse(taw.TAW_ERR_SHAPE, taw.taw_grad_norm, ok, 1.0, 1.0, far, OK, ws)
     refuse(taw.TAW_ERR_NULL, taw.taw_clip_coef, None, 1.0)
     refuse(taw.TAW_ERR_ALIGN, taw.taw_clip_coef, far + 8, 1.0)
     refuse(taw.TAW_ERR_NULL, taw.taw_grad_clip, ok, None)
