@@ -135,15 +135,16 @@ struct RowVecs {
   }
 };
 
-// exp(l - m) = exp2(l s - m s) with s = log2 e, one fused multiply-add and one exponential.  m s is exact as far as the sum of exponentials and its
-// logarithm go, since both are taken from the rounded m s.  Beyond 1e30 the values of a row are equal or further apart than any exponential reaches:
-// s = 1 does for them, and m s does not overflow.
+// exp(l - m) = exp2(l s - m s) with s = log2 e, one fused multiply-add and one exponential.  What the rounding of m s leaves out is a factor of all the
+// exponentials of a row, which its sum has too.  Up to |m| = 2^30 that factor lies within 2^-64 .. 2^64 (half a step of a product below 2^31), and with
+// it the sum of 2^24 classes; beyond it would leave fp32's range.  There s = 1 does: m s is exact, and a logit that is not m is at least 128 away from
+// it, further than any exponential reaches.
 struct Shift {
   float s, ms;
-  bool huge;
-  __device__ __forceinline__ explicit Shift(float m) : s(fabsf(m) > 1e30f ? 1.f : kLog2e), ms(m * s), huge(fabsf(m) > 1e30f) {}
+  bool far;
+  __device__ __forceinline__ explicit Shift(float m) : s(fabsf(m) > 0x1p30f ? 1.f : kLog2e), ms(m * s), far(fabsf(m) > 0x1p30f) {}
   __device__ __forceinline__ float exp(float l) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(l, s, -ms)); }
-  __device__ __forceinline__ float lse(float m, float sum) const { return huge ? m + logf(sum) : (ms + log2f(sum)) * kLn2; }
+  __device__ __forceinline__ float lse(float m, float sum) const { return far ? m + logf(sum) : (ms + log2f(sum)) * kLn2; }
 };
 
 // A vector that a row's workgroup holds.  fp32: the exponentials take the place of the logits, and are not formed a second time for the gradient (which
@@ -429,7 +430,7 @@ __global__ void __launch_bounds__(256) loss_bwd_kernel(const TL* logits, const L
   }
   const Shift sh(lse);
   const float up = none ? 0.f : dloss[t];
-  const float rest = sh.huge ? 1.f : __builtin_amdgcn_exp2f(-__builtin_fmaf(lse, sh.s, -sh.ms));     // what the rounding of lse s leaves out
+  const float rest = sh.far ? 1.f : __builtin_amdgcn_exp2f(-__builtin_fmaf(lse, sh.s, -sh.ms));     // what the rounding of lse s leaves out
   struct {
     float scale, share, own;
   } const g{up * (c.z != 0.f ? 1.f + 2.f * c.z * lse : 1.f) * rest, up * c.each, up * (1.f - c.eps)};
@@ -510,7 +511,7 @@ __global__ void __launch_bounds__(256) loss_part_kernel(const TL* __restrict__ l
 __device__ __forceinline__ float part_weight(const PartSum& p, float m) {
   if (p.m == -kInf) return 0.f;
   const Shift a(p.m), b(m);
-  return p.m == m ? 1.f : a.huge != b.huge ? (p.m > m ? kInf : 0.f) : __builtin_amdgcn_exp2f(a.ms - b.ms);
+  return p.m == m ? 1.f : a.far != b.far ? 0.f : __builtin_amdgcn_exp2f(a.ms - b.ms);      // p.m <= m: one that is far and one that is not are 128 apart
 }
 
 // joined by a wavefront, a part a lane: every lane has the result

@@ -1,0 +1,125 @@
+"""The loss over the vocabulary where logits are large, through every kernel that forms it: a workgroup for a few short rows, a wavefront and a
+workgroup to a row, rows that are longer than a workgroup holds, rows that are cut into parts, and the gradient from a saved lse.
+
+Tolerances count roundings: u = 2^-24 is half a step of fp32.  A row's probabilities depend on the differences between its logits alone, which are
+exact where the row's values are equal or neighbours; so their bounds have no term for the size of the logits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_09741_amd.binding as taw
+from oracle import model_ops as M
+from tests.test_gpu_model import DT, IDS, f64, on_gpu, scratch
+
+pytestmark = pytest.mark.gpu
+u = 2.0 ** -24
+TYPES = [("bf16", "bf16", "i64"), ("f32", "bf16", "i32"), ("f32", "f32", "i64")]
+# few rows in one launch; a wavefront a row; workgroups of 256 and 512; longer than a workgroup holds; cut into parts
+SHAPES = [(16, 40), (80, 40), (80, 3001), (80, 9001), (80, 30001), (160, 70001), (48, 70001), (80, 140003)]
+
+
+def call_loss(l, y, dtype, grad, ldt, gradient=True, **kw):
+    """(loss, rows, lse, dlogits) of logits and labels given in fp64, and the logits as stored"""
+    T, V = l.shape
+    t = on_gpu(l, DT[dtype][1])
+    d = taw.make_loss_desc(DT[dtype][0], T, V, grad_dtype=DT[grad][0], **kw)
+    loss, rows, lse = torch.full((4,), 5.0, device="cuda"), torch.full((T,), 5.0, device="cuda"), torch.full((T,), 5.0, device="cuda")
+    out = torch.full((T, V), 9.0, dtype=DT[grad][1], device="cuda")
+    labels, ws = on_gpu(y, IDS[ldt]), scratch(taw.taw_loss_workspace_bytes(d))
+    if gradient:
+        taw.taw_loss_fwd_bwd(d, t, labels, loss, rows, lse, out, ws)
+    else:
+        taw.taw_loss_fwd(d, t, labels, loss, rows, lse, ws)
+    return f64(loss), f64(rows), f64(lse), f64(out), f64(t)
+
+
+def saved(l, y, lse, w, dtype, grad, ldt, **kw):
+    T, V = l.shape
+    d = taw.make_loss_desc(DT[dtype][0], T, V, grad_dtype=DT[grad][0], **kw)
+    out = torch.full((T, V), 9.0, dtype=DT[grad][1], device="cuda")
+    taw.taw_loss_bwd(d, on_gpu(l, DT[dtype][1]), on_gpu(y, IDS[ldt]), on_gpu(lse, torch.float32), on_gpu(w, torch.float32), out)
+    return f64(out)
+
+
+def far_rows(T, V, seed):
+    """Rows around maxima of every size: uniform ones, ones with a single logit above the rest or below it, ones with most classes masked."""
+    maxima = [0.0]
+    for m in (1e4, 1e6, 1e8, 1e9, 2.0 ** 30, 2.0 ** 30 + 128, 1.25e9, 3e9, 1e10, 1e12, 1e20, 9e29, 1e30, 2e30, 1e38, 3.3e38):
+        maxima += [m, -m]
+    rng = np.random.default_rng(seed)
+    l, y = np.empty((T, V)), rng.integers(0, V, T)
+    start = rng.integers(0, len(maxima))
+    for t in range(T):
+        m, kind, c = maxima[(start + t) % len(maxima)], (t // len(maxima) + t) % 4, rng.integers(0, V)
+        l[t] = m
+        if kind == 1:                       # one above the rest; every other of them is the label
+            l[t] = m - 0.5 * abs(m) if m > -3e38 else m
+            l[t, c] = m
+            if rng.random() < 0.5:
+                y[t] = c
+        if kind == 2 and m < 3e38:          # one below the rest
+            l[t, c] = m - 0.01 * abs(m) - 1000.0
+        if kind == 3:
+            l[t, rng.random(V) < 0.9] = -np.inf
+            l[t, y[t]] = m
+    return l, y
+
+
+def near(got, want, tol, what):
+    assert np.array_equal(np.isfinite(got), np.isfinite(want)), what
+    fine = np.isfinite(want)
+    assert np.array_equal(got[~fine], want[~fine]), what
+    tol = np.broadcast_to(tol, want.shape)[fine]
+    worst = np.max(np.abs(got[fine] - want[fine]) / np.maximum(tol, 1e-300), initial=0.0)
+    assert worst <= 1.0, (what, worst)
+
+
+def gradient_bound(l, y, p, up, half, ref):
+    """Every logit here is its row's maximum or has no probability (its exponential is below e^-64).  The exponentials of the maximum are one value; their
+    sum adds a rounding for every 64 of them and a tree of 24; what is scaled, divided and subtracted has four of its size.  An exponential is held to
+    2^-62: it is formed beside a factor of up to 2^64 that it shares with the sum."""
+    T, V = l.shape
+    tol = np.abs(up)[:, None] * (p * (V / 64 + 40) * u + 2.0 ** -61)
+    tol[np.arange(T), y] += np.abs(up) * 4 * u
+    return tol + half * np.abs(ref) + 2.0 ** -133
+
+
+@pytest.mark.parametrize("T,V", SHAPES)
+@pytest.mark.parametrize("dtype,grad,ldt", TYPES)
+def test_loss_of_rows_far_from_zero(taw, T, V, dtype, grad, ldt):
+    """A maximum of any size is a finite logit like any other: loss and lse are finite, probabilities are those of the differences."""
+    l, y = far_rows(T, V, T + V)
+    l = f64(on_gpu(l, DT[dtype][1]))
+    want_rows, want_lse, counted = M.loss_fwd(l, y)
+    assert counted.all() and np.isfinite(want_lse).all()
+    up = np.full(T, 1.0 / T)
+    ref = M.loss_bwd(l, y, want_lse, up)
+    top = np.max(l, 1, keepdims=True)
+    p = np.where(l == top, 1.0, 0.0) / np.sum(l == top, 1, keepdims=True)
+    ref_p = p * up[:, None]                 # fp64 does not hold lse - l of the largest rows either
+    ref_p[np.arange(T), y] -= up
+    small = np.abs(top[:, 0]) < 1e6
+    assert np.abs(ref - ref_p)[small].max() <= 1e-8 * up[0]
+    size = np.max(np.abs(l), 1, where=np.isfinite(l), initial=0.0)
+    tol = u * (V / 64 + 128 + 8 * size)     # what is formed of logits of that size, each rounding a half step of it
+    for gradient in (False, True):
+        loss, rows, lse, out, _ = call_loss(l, y, dtype, grad, ldt, gradient)
+        near(lse, want_lse, tol, "lse")
+        near(rows, want_rows, 2 * tol, "rows")
+        assert loss[1] == T and list(loss[2:]) == [5.0, 5.0]
+    near(out, ref_p, gradient_bound(l, y, p, up, DT[grad][2], ref_p), "dlogits")
+
+
+@pytest.mark.parametrize("T,V", [(80, 40), (80, 3001), (80, 30001)])
+@pytest.mark.parametrize("dtype,grad,ldt", TYPES)
+def test_gradient_from_a_saved_lse_far_from_zero(taw, T, V, dtype, grad, ldt):
+    l, y = far_rows(T, V, T + V + 1)
+    l = f64(on_gpu(l, DT[dtype][1]))
+    lse = M.loss_fwd(l, y)[1].astype(np.float32).astype(np.float64)
+    w = np.random.default_rng(V).normal(size=T).astype(np.float32).astype(np.float64)
+    ref = M.loss_bwd(l, y, lse, w)
+    p = np.exp(np.minimum(l - lse[:, None], 0.0))
+    # the lse as saved is the formula's; a probability has the exponent's rounding (of what remains of 2^+-64 and of the difference) and three of its own
+    tol = np.abs(w)[:, None] * (p * u * (2 * 64 + 8 * np.minimum(np.abs(l - lse[:, None]), 1e3) + 16) + 2.0 ** -61)
+    tol[np.arange(T), y] += np.abs(w) * 4 * u
+    near(saved(l, y, lse, w, dtype, grad, ldt), ref, tol + DT[grad][2] * np.abs(ref) + 2.0 ** -133, "dlogits")
