@@ -142,7 +142,12 @@ struct RowVecs {
 struct Shift {
   float s, ms;
   bool far;
-  __device__ __forceinline__ explicit Shift(float m) : s(fabsf(m) > 0x1p30f ? 1.f : kLog2e), ms(m * s), far(fabsf(m) > 0x1p30f) {}
+  __device__ __forceinline__ explicit Shift(float m) {
+#pragma clang fp contract(off)        // everything rests on the rounded product: it is not to be fused with what it is added to
+    far = fabsf(m) > 0x1p30f;
+    s = far ? 1.f : kLog2e;
+    ms = m * s;
+  }
   __device__ __forceinline__ float exp(float l) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(l, s, -ms)); }
   __device__ __forceinline__ float lse(float m, float sum) const { return far ? m + logf(sum) : (ms + log2f(sum)) * kLn2; }
 };
@@ -509,6 +514,7 @@ __global__ void __launch_bounds__(256) loss_part_kernel(const TL* __restrict__ l
 
 // what a part's sum counts for beside the row's maximum m
 __device__ __forceinline__ float part_weight(const PartSum& p, float m) {
+#pragma clang fp contract(off)        // of the rounded products, as in the sums: with either unrounded, logits around 1e4 are off by up to 3e-4
   if (p.m == -kInf) return 0.f;
   const Shift a(p.m), b(m);
   return p.m == m ? 1.f : a.far != b.far ? 0.f : __builtin_amdgcn_exp2f(a.ms - b.ms);      // p.m <= m: one that is far and one that is not are 128 apart

@@ -123,3 +123,35 @@ def test_gradient_from_a_saved_lse_far_from_zero(taw, T, V, dtype, grad, ldt):
     tol = np.abs(w)[:, None] * (p * u * (2 * 64 + 8 * np.minimum(np.abs(l - lse[:, None]), 1e3) + 16) + 2.0 ** -61)
     tol[np.arange(T), y] += np.abs(w) * 4 * u
     near(saved(l, y, lse, w, dtype, grad, ldt), ref, tol + DT[grad][2] * np.abs(ref) + 2.0 ** -133, "dlogits")
+
+
+@pytest.mark.parametrize("T,V", [(3, 900), (40, 5001), (3, 20000), (160, 50001), (48, 50001), (100, 150001)])
+@pytest.mark.parametrize("grad", ["bf16", "f32"])
+@pytest.mark.parametrize("base", [1e4, -1e4, 1e6, 1e8])
+def test_parts_of_a_row_weighed_against_each_other(taw, T, V, grad, base):
+    """One logit above all the others, which are equal and have most of the sum between them: the parts of a cut row, and the wavefronts of another,
+    have different maxima, at sizes where the rounding of a maximum times log2 e is worth up to the 2^4 of the largest base."""
+    rng = np.random.default_rng(V + T)
+    step = float(np.spacing(np.float32(abs(base))))
+    l, y = np.empty((T, V)), rng.integers(0, V, T)
+    log2e = np.longdouble(np.float32(1.44269504088896340736))
+    for t in range(T):
+        at = base + step * rng.integers(-400, 400, 200)
+        product = at.astype(np.longdouble) * log2e
+        l[t] = at[np.argmax(np.abs(product - product.astype(np.float32)))]      # the roundest of some
+        l[t, rng.integers(0, V)] += max(step, round(rng.uniform(0.5, 6.0) / step) * step)
+    assert np.array_equal(l, l.astype(np.float32))
+    w = np.full(T, 1.0)
+    want_rows, want_lse, _ = M.loss_fwd(l, y)
+    loss, rows, lse, out, _ = call_loss(l, y, "f32", grad, "i64", flags=0)
+    ref = M.loss_bwd(l, y, want_lse, w) if abs(base) < 1e6 else None
+    d = l - np.max(l, 1, keepdims=True)
+    p = np.exp(d) / np.sum(np.exp(d), 1, keepdims=True)
+    want = p.copy()
+    want[np.arange(T), y] -= 1.0
+    if ref is not None:
+        assert np.abs(ref - want).max() <= 1e-10
+    # the difference's product with log2 e has two roundings and the exponential two more of its result, in the numerator and in the sum; then the sum's
+    tol = p * u * (V / 64 + 40 + 4 * np.abs(d))
+    tol[np.arange(T), y] += 4 * u
+    near(out, want, tol + DT[grad][2] * np.abs(want) + 2.0 ** -61, "dlogits")
