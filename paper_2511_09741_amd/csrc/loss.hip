@@ -149,7 +149,8 @@ struct Shift {
     ms = m * s;
   }
   __device__ __forceinline__ float exp(float l) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(l, s, -ms)); }
-  __device__ __forceinline__ float lse(float m, float sum) const { return far ? m + logf(sum) : (ms + log2f(sum)) * kLn2; }
+  // log sum exp(l - m), of the sum of exp()
+  __device__ __forceinline__ float log_sum(float m, float sum) const { return (log2f(sum) - __builtin_fmaf(m, s, -ms)) * kLn2; }
 };
 
 // A vector that a row's workgroup holds.  fp32: the exponentials take the place of the logits, and are not formed a second time for the gradient (which
@@ -179,17 +180,19 @@ __device__ __forceinline__ void gradient(const R& row, unsigned c, const typenam
   row.store(c, g);
 }
 
-// what a row comes to, from its maximum m, its sum of exponentials and (label smoothing) its weighted sum of logits; the thread that is told to stores it
+// what a row comes to, from its maximum m, its sum of exponentials and (label smoothing) its weighted sum of logits; the thread that is told to stores it.
+// The loss is the maximum less the label's logit, which is exact where they are close, and log sum exp(l - m), not lse less the logit: that would have the
+// roundings of lse, which are of the logits' size (5e-4 at 1e4).  lse is rounded once from both: it is not below a maximum of 2 or more in size.
 struct RowResult {
   float scale, share, own;                         // gradient: scale * exp(l) - share, - own at the label
   float loss = 0.f;                                // for the thread that stores it
   __device__ __forceinline__ RowResult(const Shift& sh, float m, float sum, float total, float ly, const RowTerms& c, float counted, int64_t t, bool store,
                                        float* __restrict__ rows, float* __restrict__ lse_out) {
     const bool none = sum == 0.f;                  // nothing but -inf
-    const float lse = none ? -kInf : sh.lse(m, sum);
+    const float log_sum = sh.log_sum(m, sum), lse = none ? -kInf : m + log_sum;
     if (store) {
-      float r = none ? kInf : lse - (1.f - c.eps) * ly;
-      if (c.each != 0.f) r -= total;
+      float r = none ? kInf : __builtin_fmaf(1.f - c.eps, m - ly, log_sum);
+      if (c.each != 0.f) r += __builtin_fmaf(c.eps, m, -total);
       if (c.z != 0.f) r += c.z * lse * lse;
       rows[t] = loss = r;
       if (lse_out) lse_out[t] = lse;

@@ -155,3 +155,49 @@ def test_parts_of_a_row_weighed_against_each_other(taw, T, V, grad, base):
     tol = p * u * (V / 64 + 40 + 4 * np.abs(d))
     tol[np.arange(T), y] += 4 * u
     near(out, want, tol + DT[grad][2] * np.abs(want) + 2.0 ** -61, "dlogits")
+
+
+def lse_and_rows_bound(l, V, lse, rows):
+    """A row's loss and lse are formed from its maximum m and from log sum exp(l - m), which is at most log V: that has the roundings of the sum, of the
+    exponents, and of a logarithm of up to 64 + 24 and what is taken from it; lse one more of its own size, the loss one of m - l_y and one of itself."""
+    m = np.max(l, 1)
+    low = np.min(l, 1, where=np.isfinite(l), initial=np.inf)
+    e = u * (V / 64 + 24 + 4 * np.minimum(m - low, 104.0) + 4 * 88)
+    return e + u * np.abs(lse), e + 4 * u * np.abs(rows)
+
+
+@pytest.mark.parametrize("T,V", SHAPES)
+@pytest.mark.parametrize("dtype,grad,ldt", TYPES)
+def test_loss_does_not_depend_on_where_a_row_lies(taw, T, V, dtype, grad, ldt):
+    """lse is the nearest value but for the roundings of a sum of numbers below 1, never below the maximum, and the loss keeps what lse has no room for."""
+    l, y = far_rows(T, V, T + V + 2)
+    l = f64(on_gpu(l, DT[dtype][1]))
+    rng = np.random.default_rng(V)
+    near_rows = rng.normal(0, 2, (T, V)) + rng.choice([0.0, 20.0, -300.0, 5000.0], T)[:, None]
+    for l in (l, f64(on_gpu(near_rows, DT[dtype][1]))):
+        m = np.max(l, 1)
+        log_sum = np.log(np.sum(np.exp(l - m[:, None]), 1))
+        want_lse, want_rows = m + log_sum, (m - l[np.arange(T), y]) + log_sum
+        t_lse, t_rows = lse_and_rows_bound(l, V, want_lse, want_rows)
+        for gradient in (False, True):
+            loss, rows, lse, _, _ = call_loss(l, y, dtype, grad, ldt, gradient, flags=0)
+            near(lse, want_lse, t_lse, "lse")
+            near(rows, want_rows, t_rows, "rows")
+            assert np.all(lse >= m - u * (V / 64 + 400))
+            with np.errstate(over="ignore"):
+                total = np.sum(want_rows, keepdims=True).astype(np.float32).astype(np.float64)      # more than fp32 holds: infinite
+            near(loss[:1], total, np.sum(t_rows) + 2 * u * np.abs(total), "loss")
+
+
+@pytest.mark.parametrize("T,V", [(80, 40), (80, 3001), (80, 30001)])
+@pytest.mark.parametrize("dtype,grad,ldt", TYPES)
+def test_forward_and_backward_far_from_zero(taw, T, V, dtype, grad, ldt):
+    """The gradient from the lse that the forward left: no probability is more than 1."""
+    l, y = far_rows(T, V, T + V + 3)
+    _, _, lse, _, l = call_loss(l, y, dtype, grad, ldt, False)
+    assert np.all(lse >= np.max(l, 1) - u * (V / 64 + 400))
+    w = np.full(T, 1.0)
+    out = saved(l, y, lse, w, dtype, grad, ldt)
+    p = out.copy()
+    p[np.arange(T), y] += 1.0
+    assert np.isfinite(out).all() and np.all(p <= 1.0 + 2.0 ** -7) and np.all(p >= -2.0 ** -8)
