@@ -58,7 +58,9 @@ int taw_embed_bwd(const taw_embed_desc* desc, const void* ids, int32_t id_type, 
  * such a class is the label or has a share eps/V of it, and its gradient -up times what it has of the label (0 without smoothing).
  * (The type's lowest value is a finite logit like any other.)  A counted row with nothing but -inf has lse -inf, loss +inf and a gradient of 0;
  * +inf or NaN in a counted row make all of its results NaN.
- * Everything is computed in fp32 (sums over rows in fp64) from the logits as stored, and dlogits is rounded once.
+ * Everything is computed in fp32 (sums over rows in fp64) from the logits as stored, and dlogits is rounded once.  Only differences of
+ * logits count: a row's loss and probabilities are no less exact far from zero (the sum of logits of a smoothed label, the z-loss and
+ * lse itself have the precision of numbers of their size).
  * dlogits [T, V_pad] of grad_dtype with row stride ld_grad: columns V .. V_pad-1 (a vocabulary padded for the products around
  * this call) are written as zeros; columns of logits beyond V are not read.  dlogits may be logits itself where types and strides
  * are equal. */
@@ -88,7 +90,8 @@ int taw_loss_fwd_bwd(const taw_loss_desc* desc, const void* logits, const void* 
                      float* loss_rows, float* lse, void* dlogits, void* workspace, size_t workspace_bytes, void* stream);
 
 /* The gradient from lse (as taw_loss_fwd wrote it) and the gradient of every row's loss (fp32 [T]); grad_scale and TAW_LOSS_MEAN
- * play no part. */
+ * play no part.  exp(l - lse) is formed with the lse that is given, which fp32 holds to 2^-24 of its size: around 1e4 the probabilities
+ * of a row have a common factor of up to 1 +- 5e-4, which those of taw_loss_fwd_bwd have not. */
 int taw_loss_bwd(const taw_loss_desc* desc, const void* logits, const void* labels, int32_t label_type, const float* lse,
                  const float* dloss_rows, void* dlogits, void* stream);
 

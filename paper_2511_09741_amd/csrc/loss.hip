@@ -1,7 +1,7 @@
 // Cross entropy over the vocabulary, with label smoothing and z-loss, and its gradient.
 //   lse = log sum_v exp l_v;  row = lse - (1 - eps) l_y - eps/V sum_v l_v + z lse^2
 //   dl_v = up ((1 + 2 z lse) exp(l_v - lse) - (1 - eps) [v = y] - eps/V)
-// Bound by memory: the logits are read once and the gradient is written once.
+// Bound by memory: the logits are read once (rows of more than 8192 vectors of 16 bytes twice) and the gradient is written once.
 #include <type_traits>
 
 #include "dev_common.h"
@@ -91,7 +91,9 @@ __device__ __forceinline__ void store_loss(double s, int64_t n, int mean, float*
 // =============================================================================== a row as vectors
 // A row is taken as `count` vectors of 16 bytes that are aligned in memory, whatever its first element is aligned to, and the up to VW - 1 elements
 // before and behind them, its edge, of which each of the first threads has one.  SAME: the gradient's rows start as far from a vector as the logits',
-// so that its vectors are aligned too; without it they are stored element by element.
+// so that its vectors are aligned too; without it they are stored element by element, which costs (rows of 32003 logits, us with the gradient's stride
+// 32064 and the logits' 32003 / 32064): gradient from a saved lse, 2048 rows of bf16 63 / 43; with the loss, 8192 rows of bf16 218 / 187, fp32 to bf16
+// 286 / 250, fp32 397 / 354.
 template <typename TL, typename TG, bool SAME>
 struct RowVecs {
   static constexpr int VW = 16 / sizeof(TL);
@@ -673,10 +675,12 @@ static int by_types(const LossArgs& a, F f) {
 // Rows up to which a workgroup counts the labels itself.  us so and with a launch for the count: 256 rows of 1000 7.8 and 10.3, 1024 rows of 1000 10.2 and
 // 10.4, of 32000 26.9 and 29.6; 2048 rows of 1000 13.6 and 10.3, 3000 rows of 32000 81 and 76.
 constexpr int kCountedInline = 1024;
-// Rows up to which one workgroup counts the labels, and one adds up the losses, not 64 and another launch.
 // More rows than this that a wavefront holds lie four to a workgroup: with gradient, 65536 rows of 4000 bf16 187 us (201 with a workgroup to a row), 16384 57 and 60,
 // 4096 the same.  Those of at most a vector a lane always do, with registers for no more: 2^20 rows of 256 453 us (516 with room for eight), 333 of 30 the same.
 constexpr int kWaveRows = 2047;
+// Rows up to which one workgroup counts the labels, and one adds up the losses, not 64 and another launch.  us with one and with 64, rows of 64 bf16, loss
+// alone / with gradient: 4096 rows 7.6 and 9.8 / 10.9 and 14.8, 8192 10.0 and 9.8 / 14.5 and 16.4, 16384 15.1 and 10.8 / 22.0 and 17.1, 65536 53 and 23 /
+// 74 and 36, 2^20 902 and 288.
 constexpr int kOneGroup = 16384;
 
 int launch_loss(const LossArgs& a, const void* logits, const void* labels, float* loss, float* rows, float* lse, void* dlogits, void* ws, hipStream_t st) {
