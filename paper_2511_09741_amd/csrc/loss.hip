@@ -184,7 +184,7 @@ __device__ __forceinline__ void gradient(const R& row, unsigned c, const typenam
 
 // what a row comes to, from its maximum m, its sum of exponentials and (label smoothing) its weighted sum of logits; the thread that is told to stores it.
 // The loss is the maximum less the label's logit, which is exact where they are close, and log sum exp(l - m), not lse less the logit: that would have the
-// roundings of lse, which are of the logits' size (5e-4 at 1e4).  lse is rounded once from both: it is not below a maximum of 2 or more in size.
+// roundings of lse, which are of the logits' size (5e-4 at 1e4).  lse is rounded once from both: far from zero it does not fall below the maximum.
 struct RowResult {
   float scale, share, own;                         // gradient: scale * exp(l) - share, - own at the label
   float loss = 0.f;                                // for the thread that stores it
@@ -193,7 +193,7 @@ struct RowResult {
     const bool none = sum == 0.f;                  // nothing but -inf
     const float log_sum = sh.log_sum(m, sum), lse = none ? -kInf : m + log_sum;
     if (store) {
-      float r = none ? kInf : __builtin_fmaf(1.f - c.eps, m - ly, log_sum);
+      float r = none ? kInf : __builtin_fmaf(2.f * (1.f - c.eps), 0.5f * m - 0.5f * ly, log_sum);      // halves: the whole may be more than fp32 holds
       if (c.each != 0.f) r += __builtin_fmaf(c.eps, m, -total);
       if (c.z != 0.f) r += c.z * lse * lse;
       rows[t] = loss = r;

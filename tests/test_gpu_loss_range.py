@@ -201,3 +201,20 @@ def test_forward_and_backward_far_from_zero(taw, T, V, dtype, grad, ldt):
     p = out.copy()
     p[np.arange(T), y] += 1.0
     assert np.isfinite(out).all() and np.all(p <= 1.0 + 2.0 ** -7) and np.all(p >= -2.0 ** -8)
+
+
+@pytest.mark.parametrize("T,V", [(3, 2), (40, 2), (3, 5001), (3, 70001), (160, 70001)])
+@pytest.mark.parametrize("dtype,grad,ldt", TYPES)
+def test_smoothed_loss_near_the_largest_number(taw, T, V, dtype, grad, ldt):
+    """The difference of two logits may be more than fp32 holds where the loss, which has a share of it, is not."""
+    eps = 0.5
+    l = np.full((T, V), 2e38)
+    l[:, 1] = -2.5e38 if V == 2 else -3e38
+    l = f64(on_gpu(l, DT[dtype][1]))
+    y = np.ones(T, dtype=np.int64)
+    want = M.loss_fwd(l, y, eps)[0]
+    assert np.all((want > 2e38) & (want < 3.4e38)) and np.all(l[:, 0] - l[:, 1] > 3.41e38)
+    for gradient in (False, True):
+        _, rows, _, _, _ = call_loss(l, y, dtype, grad, ldt, gradient, flags=0, label_smoothing=eps)
+        # four roundings of the loss's size, and those of the weighted sum of logits of 3e38
+        near(rows, want, u * (4 * want + eps * (V / 64 + 40) * 3e38), "rows")
